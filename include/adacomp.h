@@ -69,6 +69,10 @@ extern "C" {
 #define ADACOMP_ERR_CUDA (-7)      /* a CUDA runtime call failed */
 #define ADACOMP_ERR_UNSUPPORTED (-9) /* lazy mode: an L_T it does not take (see adacomp_compress_lazy), or flags given */
 #define ADACOMP_ERR_STATIC_SCRATCH (-8) /* adacomp_compress_static: tensor beyond the built-in scratch */
+#define ADACOMP_ERR_SHAPE (-10)    /* block operators: a size, stride, offset or bucket count outside what the call takes */
+#define ADACOMP_ERR_TYPE (-11)     /* block operators: an unknown element type, or a pair of types the call does not take */
+#define ADACOMP_ERR_VALUE (-12)    /* block operators: p not in 0..1, eps negative or not finite, scale not finite */
+#define ADACOMP_ERR_WORKSPACE (-13) /* block operators: the workspace is smaller than the _workspace call says */
 
 /* size of the scratch array built into the library for adacomp_compress_static */
 #define ADACOMP_STATIC_SCRATCH_BYTES (8u << 20)
@@ -498,6 +502,126 @@ int adacomp_stream_from_v2(const void *in_v2, void *packed_out, uint64_t out_cap
  * for production code.  (The paper has no counterpart.)
  */
 int adacomp_debug_waits(uint64_t wait_cycles, uint32_t withhold_pack_tile, uint32_t withhold_decode_item);
+
+/*
+ * Operators of a transformer block's training step.  (The paper has no counterpart: these are the layers between the
+ * matrix products whose parameters' gradients adacomp_compress* then packs.)  Dropout, layer norm with the residual add
+ * and dropout in front of it, and the attention softmax with a learned relative position bias by buckets, each forward
+ * and backward, one pass over the data.
+ *
+ * Types: activations and their gradients are binary32, bfloat16 or binary16 (`type`), arithmetic and statistics are
+ * binary32 (fused multiply-adds allowed here), each result is rounded once as it is stored.  Buffers are 16-byte aligned
+ * as everywhere (rng 8, key_len 4 bytes); rows need no alignment: any row length is taken, lengths that are multiples of
+ * 8 take 16-byte accesses.  An output may be the very buffer of an input of the same shape and type (in place); other
+ * overlaps are not allowed.  Empty tensors are valid.  Results are deterministic: the same inputs give the same bytes.
+ *
+ * Dropout.  rng: device, uint64_t[2] {seed, step}, read when the kernel runs (so a captured CUDA graph draws a new mask
+ * when the caller's step counter moves on); site: which of the model's dropouts this is.  The mask is never stored; the
+ * backward call with the same rng, site and p recomputes it.  Element (row, col) of a [rows, cols] tensor draws 16 bits of
+ * Philox4x32-10 with key = seed and counter = (col / 8, row, step mod 2^32, site): half col % 8 of the 128 bits, low half
+ * of each 32-bit word first.  With T = p * 65536 rounded to the nearest integer it is dropped when the bits are below T,
+ * otherwise multiplied by 65536 / (65536 - T).  Dropped elements become 0 whatever they held.  p = 0: no dropout (rng may
+ * be NULL in the fused calls).
+ */
+#define ADACOMP_TYPE_F32 0u
+#define ADACOMP_TYPE_BF16 1u
+#define ADACOMP_TYPE_F16 2u
+
+#define ADACOMP_MAX_NORM_COLS 65536u  /* columns of a layer norm */
+#define ADACOMP_MAX_KEYS 131072u      /* keys of a softmax row */
+#define ADACOMP_MAX_BUCKETS 128u      /* buckets of a relative position bias, both sides together */
+#define ADACOMP_MAX_DISTANCE 1024u    /* its max_distance */
+
+/* y = dropout(x) over [rows, cols]; the backward pass is the same call with dy for x. */
+int adacomp_dropout(const void *x, void *y, uint64_t rows, uint32_t cols, uint32_t type, float p, const uint64_t *rng,
+                    uint32_t site, void *stream);
+
+typedef struct adacomp_norm_options {
+    uint64_t rows;
+    uint32_t cols;          /* 1 .. ADACOMP_MAX_NORM_COLS */
+    uint32_t type;          /* of x, residual, h, y and their gradients */
+    uint32_t param_type;    /* of weight, bias and their gradients: ADACOMP_TYPE_F32, or `type` */
+    float eps;
+    float p;                /* dropout of x in front of the residual add */
+    uint32_t site;
+    const uint64_t *rng;
+} adacomp_norm_options;
+
+/*
+ * h = residual + dropout(x),  y = (h - mean) * rstd * weight + bias  over each row,  rstd = 1 / sqrt(var + eps) with the
+ * biased variance.
+ *   residual      may be NULL (h = dropout(x)); weight NULL: 1; bias NULL: 0
+ *   h_out         [rows, cols], may be NULL; what the backward call reads (without residual and dropout: x itself)
+ *   mean, rstd    float[rows] for the backward call, may be NULL
+ */
+int adacomp_layer_norm(const void *x, const void *residual, const void *weight, const void *bias, void *h_out, void *y,
+                       float *mean, float *rstd, const adacomp_norm_options *opt, void *stream);
+
+/* Bytes of `workspace` for the backward call (0: cols not taken).  Host only. */
+size_t adacomp_layer_norm_workspace(uint64_t rows, uint32_t cols);
+
+/*
+ * The gradients of adacomp_layer_norm.
+ *   dh_in         [rows, cols], may be NULL: the gradient that reaches h from elsewhere (the residual stream)
+ *   dresidual     [rows, cols], may be NULL: dh_in + the norm's gradient of h
+ *   dx            [rows, cols], may be NULL: dropout's backward of dresidual (without dropout the same values)
+ *   dweight, dbias  [cols], may be NULL: overwritten with the sums over the rows (0 for no rows)
+ * opt->p, rng and site as in the forward call.  workspace: device, needed for dweight or dbias, contents irrelevant.
+ */
+int adacomp_layer_norm_backward(const void *dy, const void *dh_in, const void *h, const void *weight, const float *mean,
+                                const float *rstd, void *dx, void *dresidual, void *dweight, void *dbias, void *workspace,
+                                size_t workspace_bytes, const adacomp_norm_options *opt, void *stream);
+
+/*
+ * Buckets of a relative position bias.  The distance of a key from a query falls into `side` buckets per side
+ * (bidirectional: num_buckets / 2 for keys up to the query's position, as many for keys behind it; else num_buckets, keys
+ * behind it counting as distance 0): the first side / 2 hold one distance each, the others are spaced by equal ratios up
+ * to max_distance, and everything farther belongs to the last.  first[k]: the smallest distance of bucket k or above.
+ * Filled by adacomp_relpos_plan (host only), kept by the caller.
+ */
+typedef struct adacomp_relpos {
+    uint32_t num_buckets, max_distance, bidirectional, side;
+    uint16_t first[ADACOMP_MAX_BUCKETS];
+} adacomp_relpos;
+
+int adacomp_relpos_plan(uint32_t num_buckets, uint32_t max_distance, uint32_t bidirectional, adacomp_relpos *plan);
+
+typedef struct adacomp_softmax_options {
+    uint32_t batch, heads, q_len, k_len;    /* k_len <= ADACOMP_MAX_KEYS */
+    uint64_t ld;            /* elements from one row to the next, >= k_len; rows are otherwise dense */
+    uint32_t type;
+    float scale;
+    uint32_t causal;        /* non-zero: query i keeps keys up to i + q_offset */
+    int32_t q_offset;       /* position of query 0 among the keys, |q_offset| <= 2^30 */
+    const int32_t *key_len; /* device, int32_t[batch], may be NULL: keys of each sequence (clamped to 0 .. k_len) */
+    float p;                /* dropout of the probabilities; its rows are (batch, head, query), its columns the keys */
+    uint32_t site;
+    const uint64_t *rng;
+} adacomp_softmax_options;
+
+/*
+ * probs = dropout(softmax(scale * scores + table[bucket(key - (query + q_offset)), head])) over the kept keys, 0 at the
+ * others, whatever their scores hold.  A row that keeps no key, or only keys whose logit is -inf, becomes zeros.
+ *   scores, probs [batch, heads, q_len, k_len], ld elements from row to row (columns k_len .. ld - 1 are neither used nor
+ *                 written; with ld a multiple of 8 they may be read)
+ *   table         float[num_buckets, heads], may be NULL (no bias; relpos is then not read)
+ *   lse           float[batch, heads, q_len], may be NULL: log of the row's sum of exponentials (-inf: nothing kept)
+ * A single new token is q_len = 1 with q_offset its position.
+ */
+int adacomp_bias_softmax(const void *scores, const float *table, const adacomp_relpos *relpos, void *probs, float *lse,
+                         const adacomp_softmax_options *opt, void *stream);
+
+/* Bytes of `workspace` for the backward call with dtable (0: sizes not taken).  Host only. */
+size_t adacomp_bias_softmax_workspace(uint32_t batch, uint32_t heads, uint32_t q_len, uint32_t k_len,
+                                      const adacomp_relpos *relpos);
+
+/*
+ * The gradients of adacomp_bias_softmax: dscores (0 where masked) and, unless NULL, dtable (overwritten; summed over the
+ * batch, the queries and the keys of each bucket).  lse is the forward call's.
+ */
+int adacomp_bias_softmax_backward(const void *dprobs, const void *scores, const float *table, const adacomp_relpos *relpos,
+                                  const float *lse, void *dscores, float *dtable, void *workspace, size_t workspace_bytes,
+                                  const adacomp_softmax_options *opt, void *stream);
 
 /* Enqueues a clear of the sticky bits on `stream`. */
 int adacomp_device_status_reset(void *stream);

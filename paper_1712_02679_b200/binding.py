@@ -46,7 +46,29 @@ class adacomp_options(C.Structure):
 
 ADACOMP_GRAD_F32, ADACOMP_GRAD_BF16, ADACOMP_GRAD_F16 = 0, 1, 2
 ADACOMP_QUANT_BIN_MAX_MEAN, ADACOMP_QUANT_SENT_MEAN = 0, 1
+ADACOMP_TYPE_F32, ADACOMP_TYPE_BF16, ADACOMP_TYPE_F16 = 0, 1, 2
+ADACOMP_MAX_NORM_COLS, ADACOMP_MAX_KEYS, ADACOMP_MAX_BUCKETS, ADACOMP_MAX_DISTANCE = 65536, 131072, 128, 1024
 _GRAD_DTYPES = {ADACOMP_GRAD_F32: torch.float32, ADACOMP_GRAD_BF16: torch.bfloat16, ADACOMP_GRAD_F16: torch.float16}
+
+_TYPES = {torch.float32: ADACOMP_TYPE_F32, torch.bfloat16: ADACOMP_TYPE_BF16, torch.float16: ADACOMP_TYPE_F16}
+
+
+class adacomp_norm_options(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("cols", C.c_uint32), ("type", C.c_uint32), ("param_type", C.c_uint32),
+                ("eps", C.c_float), ("p", C.c_float), ("site", C.c_uint32), ("rng", C.c_void_p)]
+
+
+class adacomp_relpos(C.Structure):
+    _fields_ = [("num_buckets", C.c_uint32), ("max_distance", C.c_uint32), ("bidirectional", C.c_uint32),
+                ("side", C.c_uint32), ("first", C.c_uint16 * ADACOMP_MAX_BUCKETS)]
+
+
+class adacomp_softmax_options(C.Structure):
+    _fields_ = [("batch", C.c_uint32), ("heads", C.c_uint32), ("q_len", C.c_uint32), ("k_len", C.c_uint32),
+                ("ld", C.c_uint64), ("type", C.c_uint32), ("scale", C.c_float), ("causal", C.c_uint32),
+                ("q_offset", C.c_int32), ("key_len", C.c_void_p), ("p", C.c_float), ("site", C.c_uint32),
+                ("rng", C.c_void_p)]
+
 
 _lib: Optional[C.CDLL] = None
 
@@ -140,6 +162,19 @@ def lib() -> C.CDLL:
         L.adacomp_device_status.argtypes = [C.c_void_p, C.c_void_p]
         L.adacomp_device_status_reset.restype = C.c_int
         L.adacomp_device_status_reset.argtypes = [C.c_void_p]
+        vp, u64, u32 = C.c_void_p, C.c_uint64, C.c_uint32
+        norm, soft, rel = C.POINTER(adacomp_norm_options), C.POINTER(adacomp_softmax_options), C.POINTER(adacomp_relpos)
+        for name, restype, argtypes in [
+                ("adacomp_dropout", C.c_int, [vp, vp, u64, u32, u32, C.c_float, vp, u32, vp]),
+                ("adacomp_layer_norm", C.c_int, [vp] * 8 + [norm, vp]),
+                ("adacomp_layer_norm_workspace", C.c_size_t, [u64, u32]),
+                ("adacomp_layer_norm_backward", C.c_int, [vp] * 11 + [C.c_size_t, norm, vp]),
+                ("adacomp_relpos_plan", C.c_int, [u32, u32, u32, rel]),
+                ("adacomp_bias_softmax", C.c_int, [vp, vp, rel, vp, vp, soft, vp]),
+                ("adacomp_bias_softmax_workspace", C.c_size_t, [u32, u32, u32, u32, rel]),
+                ("adacomp_bias_softmax_backward", C.c_int, [vp, vp, vp, rel, vp, vp, vp, vp, C.c_size_t, soft, vp])]:
+            f = getattr(L, name)
+            f.restype, f.argtypes = restype, argtypes
         _lib = L
     return _lib
 
@@ -525,3 +560,156 @@ def adacomp_debug_waits(wait_cycles: int = 0, withhold_pack_tile: int = 0, withh
 
 def adacomp_device_status_reset(stream=None) -> None:
     _check(lib().adacomp_device_status_reset(_stream(stream)), "adacomp_device_status_reset")
+
+
+# ---- operators of a transformer block (see include/adacomp.h) ----
+
+def _type_of(t: torch.Tensor, what: str) -> int:
+    if t.dtype not in _TYPES:
+        raise ValueError(f"{what} must be float32, bfloat16 or float16")
+    return _TYPES[t.dtype]
+
+
+def _like(t: Optional[torch.Tensor], what: str, shape, dtype) -> Optional[int]:
+    """Pointer of a dense CUDA tensor of this shape and type (None: NULL)."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    return _dev_ptr(t, what, dtype)
+
+
+def _rng_ptr(rng: Optional[torch.Tensor]) -> Optional[int]:
+    """rng: int64[2] CUDA tensor {seed, step}."""
+    return None if rng is None else _like(rng, "rng", (2,), torch.int64)
+
+
+def _rows_cols(x: torch.Tensor, what: str):
+    if x.dim() == 0:
+        raise ValueError(f"{what} needs at least one dimension")
+    cols = x.shape[-1]
+    return (x.numel() // cols if cols else 0), cols
+
+
+def adacomp_dropout(x, y, p: float, rng, site: int = 0, stream=None) -> None:
+    """y = dropout(x), rows being all dimensions but the last; the backward pass is the same call on dy."""
+    rows, cols = _rows_cols(x, "x")
+    _check(lib().adacomp_dropout(_dev_ptr(x, "x"), _like(y, "y", x.shape, x.dtype), rows, cols, _type_of(x, "x"),
+                                 float(p), _rng_ptr(rng), int(site), _stream(stream)), "adacomp_dropout")
+
+
+def _norm_options(x, params, eps, p, rng, site):
+    rows, cols = _rows_cols(x, "x")
+    kinds = {t.dtype for t in params if t is not None}
+    if len(kinds) > 1:
+        raise ValueError("weight, bias and their gradients must have one dtype")
+    kind = _type_of(next(t for t in params if t is not None), "weight") if kinds else ADACOMP_TYPE_F32
+    return adacomp_norm_options(rows, cols, _type_of(x, "x"), kind, float(eps), float(p), int(site), _rng_ptr(rng))
+
+
+def adacomp_layer_norm(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-5, residual=None, h_out=None,
+                       p: float = 0.0, rng=None, site: int = 0, stream=None) -> None:
+    """h = residual + dropout(x); y = layer_norm(h) * weight + bias over the last dimension.  mean, rstd: float32, one
+    per row, for the backward call."""
+    opt = _norm_options(x, (weight, bias), eps, p, rng, site)
+    vec, stat = (opt.cols,), x.shape[:-1]
+    kind = weight.dtype if weight is not None else None
+    _check(lib().adacomp_layer_norm(
+        _dev_ptr(x, "x"), _like(residual, "residual", x.shape, x.dtype), _like(weight, "weight", vec, kind),
+        _like(bias, "bias", vec, bias.dtype if bias is not None else None), _like(h_out, "h_out", x.shape, x.dtype),
+        _like(y, "y", x.shape, x.dtype), _like(mean, "mean", stat, torch.float32), _like(rstd, "rstd", stat, torch.float32),
+        C.byref(opt), _stream(stream)), "adacomp_layer_norm")
+
+
+def adacomp_layer_norm_workspace(rows: int, cols: int) -> int:
+    """Bytes of the workspace tensor (uint8, CUDA) of adacomp_layer_norm_backward."""
+    return int(lib().adacomp_layer_norm_workspace(int(rows), int(cols)))
+
+
+def adacomp_layer_norm_backward(dy, h, weight, mean, rstd, dx, dweight=None, dbias=None, workspace=None, dh_in=None,
+                                dresidual=None, p: float = 0.0, rng=None, site: int = 0, stream=None) -> None:
+    """Gradients of adacomp_layer_norm; any output may be None.  dh_in: the gradient reaching h from elsewhere."""
+    opt = _norm_options(h, (weight, dweight, dbias), 0.0, p, rng, site)
+    vec, stat, n = (opt.cols,), h.shape[:-1], h.shape
+    param = next((t.dtype for t in (weight, dweight, dbias) if t is not None), None)
+    _check(lib().adacomp_layer_norm_backward(
+        _like(dy, "dy", n, h.dtype), _like(dh_in, "dh_in", n, h.dtype), _dev_ptr(h, "h"), _like(weight, "weight", vec, param),
+        _like(mean, "mean", stat, torch.float32), _like(rstd, "rstd", stat, torch.float32), _like(dx, "dx", n, h.dtype),
+        _like(dresidual, "dresidual", n, h.dtype), _like(dweight, "dweight", vec, param), _like(dbias, "dbias", vec, param),
+        _dev_ptr(workspace, "workspace", torch.uint8), workspace.numel() if workspace is not None else 0, C.byref(opt),
+        _stream(stream)), "adacomp_layer_norm_backward")
+
+
+def adacomp_relpos_plan(num_buckets: int, max_distance: int, bidirectional: bool = True) -> adacomp_relpos:
+    """The buckets of a relative position bias, kept by the caller and given to the softmax calls."""
+    plan = adacomp_relpos()
+    _check(lib().adacomp_relpos_plan(int(num_buckets), int(max_distance), int(bool(bidirectional)), C.byref(plan)),
+           "adacomp_relpos_plan")
+    return plan
+
+
+def _row_stride(t: torch.Tensor, what: str) -> Optional[int]:
+    """Elements between the rows of a [batch, heads, q, k] tensor whose rows are evenly spaced (None: a single row)."""
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a CUDA tensor (no CPU path exists)")
+    if t.dim() != 4:
+        raise ValueError(f"{what} must be [batch, heads, queries, keys]")
+    if t.numel() == 0:
+        return None
+    inner, ld = 1, None
+    for dim in (2, 1, 0):
+        if t.shape[dim] > 1:
+            if ld is None:
+                ld = t.stride(dim) // inner
+            if t.stride(dim) != inner * ld:
+                raise ValueError(f"{what}: the rows must be evenly spaced")
+        inner *= t.shape[dim]
+    if t.shape[3] > 1 and t.stride(3) != 1:
+        raise ValueError(f"{what}: the keys of a row must be contiguous")
+    return ld
+
+
+def _softmax_call(scores, table, relpos, others, scale, causal, q_offset, key_len, p, rng, site):
+    """Options of a softmax call and the table's pointer; `others`: (tensor, name) of the scores' shape."""
+    ld = _row_stride(scores, "scores")
+    for t, what in others:
+        if t.shape != scores.shape or t.dtype != scores.dtype:
+            raise ValueError(f"{what} must have the shape and dtype of scores")
+        if _row_stride(t, what) != ld:
+            raise ValueError(f"{what} must have the row stride of scores")
+    b, h, q, k = scores.shape
+    if table is not None and relpos is None:
+        raise ValueError("a bias table needs its buckets (adacomp_relpos_plan)")
+    tp = _like(table, "table", (relpos.num_buckets, h), torch.float32) if table is not None else None
+    opt = adacomp_softmax_options(b, h, q, k, ld if ld is not None else k, _type_of(scores, "scores"), float(scale),
+                                  int(bool(causal)), int(q_offset), _like(key_len, "key_len", (b,), torch.int32), float(p),
+                                  int(site), _rng_ptr(rng))
+    return opt, tp, C.byref(relpos) if table is not None else None
+
+
+def adacomp_bias_softmax(scores, table, relpos: Optional[adacomp_relpos], probs, lse=None, scale: float = 1.0,
+                         causal: bool = False, q_offset: int = 0, key_len=None, p: float = 0.0, rng=None, site: int = 0,
+                         stream=None) -> None:
+    """probs = dropout(softmax(scale * scores + bias)) over [batch, heads, queries, keys]; rows may be spaced apart."""
+    opt, tp, rel = _softmax_call(scores, table, relpos, [(probs, "probs")], scale, causal, q_offset, key_len, p, rng, site)
+    _check(lib().adacomp_bias_softmax(scores.data_ptr(), tp, rel, probs.data_ptr(),
+                                      _like(lse, "lse", scores.shape[:3], torch.float32), C.byref(opt), _stream(stream)),
+           "adacomp_bias_softmax")
+
+
+def adacomp_bias_softmax_workspace(batch: int, heads: int, q_len: int, k_len: int, relpos: adacomp_relpos) -> int:
+    """Bytes of the workspace tensor (uint8, CUDA) of adacomp_bias_softmax_backward."""
+    return int(lib().adacomp_bias_softmax_workspace(int(batch), int(heads), int(q_len), int(k_len), C.byref(relpos)))
+
+
+def adacomp_bias_softmax_backward(dprobs, scores, table, relpos: Optional[adacomp_relpos], lse, dscores, dtable=None,
+                                  workspace=None, scale: float = 1.0, causal: bool = False, q_offset: int = 0, key_len=None,
+                                  p: float = 0.0, rng=None, site: int = 0, stream=None) -> None:
+    """Gradients of adacomp_bias_softmax: dscores and, unless None, the bias table's."""
+    opt, tp, rel = _softmax_call(scores, table, relpos, [(dprobs, "dprobs"), (dscores, "dscores")], scale, causal, q_offset,
+                                 key_len, p, rng, site)
+    _check(lib().adacomp_bias_softmax_backward(
+        dprobs.data_ptr(), scores.data_ptr(), tp, rel, _like(lse, "lse", scores.shape[:3], torch.float32),
+        dscores.data_ptr(), _like(dtable, "dtable", table.shape if table is not None else (), torch.float32),
+        _dev_ptr(workspace, "workspace", torch.uint8), workspace.numel() if workspace is not None else 0, C.byref(opt),
+        _stream(stream)), "adacomp_bias_softmax_backward")

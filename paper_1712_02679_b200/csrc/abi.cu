@@ -59,6 +59,10 @@ const char *adacomp_strerror(int code)
     case ADACOMP_ERR_UNSUPPORTED: return "lazy mode supports L_T = 41..1000 (and multiples of 4 up to 4000) without flags only";
     case ADACOMP_ERR_STATIC_SCRATCH:
         return "tensor needs more scratch than the library's built-in array holds; use adacomp_compress";
+    case ADACOMP_ERR_SHAPE: return "a size, stride, offset or bucket count is outside what the call takes";
+    case ADACOMP_ERR_TYPE: return "unknown element type, or a pair of types the call does not take";
+    case ADACOMP_ERR_VALUE: return "p must be in 0..1, eps finite and not negative, scale finite";
+    case ADACOMP_ERR_WORKSPACE: return "the workspace is smaller than the workspace call says";
     default: return "unknown error code";
     }
 }

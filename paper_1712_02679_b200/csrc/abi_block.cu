@@ -1,0 +1,245 @@
+// C ABI of the operators of a transformer block (include/adacomp.h): argument checks, then the launchers in dropout.cu,
+// norm*.cu and softmax*.cu.
+#include <math.h>
+#include <initializer_list>
+
+#include "block.h"
+
+namespace adacomp_impl {
+
+int launched() { return cudaGetLastError() == cudaSuccess ? ADACOMP_OK : ADACOMP_ERR_CUDA; }
+
+bool drop_args(float p, const void *rng, uint32_t site, DropArgs &out)
+{
+    if (!(p >= 0.f && p <= 1.f)) return false;
+    out.rng = static_cast<const u64 *>(rng);
+    out.site = site;
+    out.threshold = (u32)lrintf(p * 65536.f);
+    out.factor = out.threshold == 65536u ? 0.f : 65536.f / (float)(65536u - out.threshold);
+    return true;
+}
+
+static bool misaligned_any(std::initializer_list<const void *> ps)
+{
+    for (const void *p : ps)
+        if (misaligned(p)) return true;
+    return false;
+}
+
+static int check_drop(float p, const uint64_t *rng, uint32_t site, DropArgs &out)
+{
+    if (!drop_args(p, rng, site, out)) return ADACOMP_ERR_VALUE;
+    if (out.threshold && !rng) return ADACOMP_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(rng) & 7u) return ADACOMP_ERR_ALIGN;
+    return ADACOMP_OK;
+}
+
+// What the forward and the backward call of layer norm check alike.
+static int check_norm(const adacomp_norm_options *opt, NormArgs &a)
+{
+    if (!opt) return ADACOMP_ERR_NULL;
+    if (opt->type > ADACOMP_TYPE_F16 || opt->param_type > ADACOMP_TYPE_F16) return ADACOMP_ERR_TYPE;
+    if (opt->param_type != ADACOMP_TYPE_F32 && opt->param_type != opt->type) return ADACOMP_ERR_TYPE;
+    if (opt->cols == 0 || opt->cols > ADACOMP_MAX_NORM_COLS || opt->rows >= (1ull << 32)) return ADACOMP_ERR_SHAPE;
+    if (!(opt->eps >= 0.f) || isinf(opt->eps)) return ADACOMP_ERR_VALUE;
+    a.rows = opt->rows;
+    a.cols = opt->cols;
+    a.param_type = opt->param_type;
+    a.eps = opt->eps;
+    return check_drop(opt->p, opt->rng, opt->site, a.drop);
+}
+
+static int check_softmax(const float *table, const adacomp_relpos *relpos, const adacomp_softmax_options *opt,
+                         SoftmaxArgs &a)
+{
+    if (!opt) return ADACOMP_ERR_NULL;
+    if (opt->type > ADACOMP_TYPE_F16) return ADACOMP_ERR_TYPE;
+    const u64 heads = (u64)opt->batch * opt->heads;
+    if (opt->k_len > ADACOMP_MAX_KEYS || opt->ld < opt->k_len || opt->q_len >= (1u << 30) || opt->q_offset > (1 << 30) ||
+        opt->q_offset < -(1 << 30) || heads >= (1ull << 32) || (opt->q_len && heads >= (1ull << 32) / opt->q_len))
+        return ADACOMP_ERR_SHAPE;
+    if (!isfinite(opt->scale)) return ADACOMP_ERR_VALUE;
+    a.batch = opt->batch;
+    a.heads = opt->heads;
+    a.q_len = opt->q_len;
+    a.k_len = opt->k_len;
+    a.ld = opt->ld;
+    a.scale = opt->scale;
+    a.causal = opt->causal;
+    a.q_offset = opt->q_offset;
+    a.key_len = opt->key_len;
+    a.table = table;
+    a.reach = a.both = 0;
+    a.side = a.buckets = 1;
+    a.first[0] = 0;
+    if (table) {
+        if (!relpos) return ADACOMP_ERR_NULL;
+        const u32 sides = relpos->bidirectional ? 2u : 1u;
+        if (relpos->num_buckets > ADACOMP_MAX_BUCKETS || relpos->side < 2 || relpos->side * sides != relpos->num_buckets ||
+            relpos->max_distance > ADACOMP_MAX_DISTANCE || relpos->first[0] != 0)
+            return ADACOMP_ERR_SHAPE;
+        for (u32 k = 0; k < relpos->side; k++) {
+            a.first[k] = relpos->first[k];
+            if (k && a.first[k] < a.first[k - 1]) return ADACOMP_ERR_SHAPE;
+        }
+        a.side = relpos->side;
+        a.buckets = relpos->num_buckets;
+        a.both = sides == 2u;
+        a.reach = a.first[a.side - 1];
+        if (a.reach < 1 || a.reach > ADACOMP_MAX_DISTANCE) return ADACOMP_ERR_SHAPE;
+    }
+    if ((reinterpret_cast<uintptr_t>(opt->key_len) | reinterpret_cast<uintptr_t>(table)) & 3u) return ADACOMP_ERR_ALIGN;
+    return check_drop(opt->p, opt->rng, opt->site, a.drop);
+}
+
+}  // namespace adacomp_impl
+
+using namespace adacomp_impl;
+
+extern "C" {
+
+int adacomp_dropout(const void *x, void *y, uint64_t rows, uint32_t cols, uint32_t type, float p, const uint64_t *rng,
+                    uint32_t site, void *stream)
+{
+    if (type > ADACOMP_TYPE_F16) return ADACOMP_ERR_TYPE;
+    if (rows >= (1ull << 32)) return ADACOMP_ERR_SHAPE;
+    DropArgs drop;
+    if (!drop_args(p, rng, site, drop)) return ADACOMP_ERR_VALUE;
+    if (rows == 0 || cols == 0) return ADACOMP_OK;
+    if (!x || !y || !rng) return ADACOMP_ERR_NULL;
+    if (misaligned_any({x, y}) || (reinterpret_cast<uintptr_t>(rng) & 7u)) return ADACOMP_ERR_ALIGN;
+    return launch_dropout(x, y, rows, cols, type, drop, static_cast<cudaStream_t>(stream));
+}
+
+int adacomp_layer_norm(const void *x, const void *residual, const void *weight, const void *bias, void *h_out, void *y,
+                       float *mean, float *rstd, const adacomp_norm_options *opt, void *stream)
+{
+    NormArgs a = {};
+    const int rc = check_norm(opt, a);
+    if (rc != ADACOMP_OK) return rc;
+    if (a.rows == 0) return ADACOMP_OK;
+    if (!x || !y) return ADACOMP_ERR_NULL;
+    if (misaligned_any({x, residual, weight, bias, h_out, y, mean, rstd})) return ADACOMP_ERR_ALIGN;
+    a.x = x;
+    a.residual = residual;
+    a.weight = weight;
+    a.bias = bias;
+    a.h = h_out;
+    a.y = y;
+    a.mean = mean;
+    a.rstd = rstd;
+    return launch_norm(a, opt->type, static_cast<cudaStream_t>(stream));
+}
+
+size_t adacomp_layer_norm_workspace(uint64_t rows, uint32_t cols)
+{
+    if (cols == 0 || cols > ADACOMP_MAX_NORM_COLS) return 0;
+    NormArgs a = {};
+    a.rows = rows;
+    a.cols = cols;
+    norm_split(a);
+    return (size_t)(a.partials ? a.partials : 1u) * 2 * cols * sizeof(float);
+}
+
+int adacomp_layer_norm_backward(const void *dy, const void *dh_in, const void *h, const void *weight, const float *mean,
+                                const float *rstd, void *dx, void *dresidual, void *dweight, void *dbias, void *workspace,
+                                size_t workspace_bytes, const adacomp_norm_options *opt, void *stream)
+{
+    NormArgs a = {};
+    const int rc = check_norm(opt, a);
+    if (rc != ADACOMP_OK) return rc;
+    if (a.rows && (!dy || !h || !mean || !rstd)) return ADACOMP_ERR_NULL;
+    if (misaligned_any({dy, dh_in, h, weight, mean, rstd, dx, dresidual, dweight, dbias, workspace})) return ADACOMP_ERR_ALIGN;
+    if (dweight || dbias) {
+        if (!workspace) return ADACOMP_ERR_NULL;
+        if (workspace_bytes < adacomp_layer_norm_workspace(a.rows, a.cols)) return ADACOMP_ERR_WORKSPACE;
+    }
+    a.dy = dy;
+    a.dh_in = dh_in;
+    a.x = h;
+    a.weight = weight;
+    a.mean = const_cast<float *>(mean);
+    a.rstd = const_cast<float *>(rstd);
+    a.dx = dx;
+    a.dresidual = dresidual;
+    a.dweight = dweight;
+    a.dbias = dbias;
+    a.partial = static_cast<float *>(workspace);
+    return launch_norm_back(a, opt->type, static_cast<cudaStream_t>(stream));
+}
+
+int adacomp_relpos_plan(uint32_t num_buckets, uint32_t max_distance, uint32_t bidirectional, adacomp_relpos *plan)
+{
+    if (!plan) return ADACOMP_ERR_NULL;
+    const u32 sides = bidirectional ? 2u : 1u, side = num_buckets / sides, exact = side / 2u;
+    if (num_buckets > ADACOMP_MAX_BUCKETS || num_buckets % sides || side < 2 || max_distance <= exact ||
+        max_distance > ADACOMP_MAX_DISTANCE)
+        return ADACOMP_ERR_SHAPE;
+    plan->num_buckets = num_buckets;
+    plan->max_distance = max_distance;
+    plan->bidirectional = bidirectional ? 1u : 0u;
+    plan->side = side;
+    for (u32 k = 0; k < ADACOMP_MAX_BUCKETS; k++) plan->first[k] = 0;
+    for (u32 k = 0; k < side; k++) {
+        if (k <= exact) {
+            plan->first[k] = (uint16_t)k;
+        } else {        // distances that the formula hits exactly belong to the bucket above: lean down by a rounding's worth
+            const double at = exact * pow((double)max_distance / exact, (double)(k - exact) / (side - exact));
+            plan->first[k] = (uint16_t)ceil(at * (1.0 - 1e-9));
+        }
+    }
+    return ADACOMP_OK;
+}
+
+int adacomp_bias_softmax(const void *scores, const float *table, const adacomp_relpos *relpos, void *probs, float *lse,
+                         const adacomp_softmax_options *opt, void *stream)
+{
+    SoftmaxArgs a = {};
+    const int rc = check_softmax(table, relpos, opt, a);
+    if (rc != ADACOMP_OK) return rc;
+    const bool any = (u64)a.batch * a.heads * a.q_len * a.k_len != 0;
+    if (any && (!scores || !probs)) return ADACOMP_ERR_NULL;
+    if (misaligned_any({scores, probs, lse})) return ADACOMP_ERR_ALIGN;
+    a.scores = scores;
+    a.probs = probs;
+    a.lse = lse;
+    return launch_softmax(a, opt->type, static_cast<cudaStream_t>(stream));
+}
+
+size_t adacomp_bias_softmax_workspace(uint32_t batch, uint32_t heads, uint32_t q_len, uint32_t k_len,
+                                      const adacomp_relpos *relpos)
+{
+    if (!relpos || k_len > ADACOMP_MAX_KEYS || relpos->num_buckets > ADACOMP_MAX_BUCKETS) return 0;
+    SoftmaxArgs a = {};
+    a.batch = batch;
+    a.heads = heads;
+    a.q_len = q_len;
+    a.k_len = k_len;
+    softmax_split(a);
+    const size_t bytes = (size_t)batch * heads * a.chunks * a.cluster * relpos->num_buckets * sizeof(float);
+    return bytes ? bytes : 16;
+}
+
+int adacomp_bias_softmax_backward(const void *dprobs, const void *scores, const float *table, const adacomp_relpos *relpos,
+                                  const float *lse, void *dscores, float *dtable, void *workspace, size_t workspace_bytes,
+                                  const adacomp_softmax_options *opt, void *stream)
+{
+    SoftmaxArgs a = {};
+    const int rc = check_softmax(table, relpos, opt, a);
+    if (rc != ADACOMP_OK) return rc;
+    const bool rows = (u64)a.batch * a.heads * a.q_len != 0;
+    if (rows && (!lse || (a.k_len && (!dprobs || !scores || !dscores)))) return ADACOMP_ERR_NULL;
+    if (dtable && (!table || !workspace)) return ADACOMP_ERR_NULL;
+    if (misaligned_any({dprobs, scores, lse, dscores, dtable, workspace})) return ADACOMP_ERR_ALIGN;
+    if (dtable && workspace_bytes < adacomp_bias_softmax_workspace(a.batch, a.heads, a.q_len, a.k_len, relpos))
+        return ADACOMP_ERR_WORKSPACE;
+    a.dprobs = dprobs;
+    a.scores = scores;
+    a.lse = const_cast<float *>(lse);
+    a.dscores = dscores;
+    a.dtable = dtable;
+    a.partial = static_cast<float *>(workspace);
+    return launch_softmax_back(a, opt->type, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,59 @@
+// Host-side declarations of the operators of a transformer block: checked arguments in, kernels enqueued.
+#pragma once
+
+#include "block.cuh"
+
+namespace adacomp_impl {
+
+// Dropout's threshold and factor of a probability; false: not a probability.
+bool drop_args(float p, const void *rng, uint32_t site, DropArgs &out);
+
+int launched();        // ADACOMP_OK, or ADACOMP_ERR_CUDA when the last launch failed
+
+// dropout.cu
+int launch_dropout(const void *x, void *y, u64 rows, u32 cols, u32 type, const DropArgs &drop, cudaStream_t st);
+
+struct NormArgs {
+    const void *x, *residual, *weight, *bias;    // forward (backward: x holds h)
+    void *h, *y;
+    float *mean, *rstd;
+    const void *dy, *dh_in;                      // backward
+    void *dx, *dresidual, *dweight, *dbias;
+    float *partial;                              // [partials][2][cols]: sums of each CTA's rows
+    u64 rows;
+    u32 cols, param_type;
+    u32 tpr, groups, cluster, slice, partials;   // norm_split: threads per row, rows per CTA, CTAs per row, columns per CTA
+    float eps;
+    DropArgs drop;
+};
+
+// norm.cu, norm_back.cu
+int launch_norm(NormArgs &a, u32 type, cudaStream_t st);
+int launch_norm_back(NormArgs &a, u32 type, cudaStream_t st);
+void norm_split(NormArgs &a);
+
+struct SoftmaxArgs {
+    const void *scores;
+    const float *table;
+    const int *key_len;
+    void *probs;                                 // forward
+    float *lse;
+    const void *dprobs;                          // backward
+    void *dscores;
+    float *dtable, *partial;                     // [batch * heads * chunks][buckets]
+    u64 ld;
+    u32 batch, heads, q_len, k_len, causal;
+    int q_offset;
+    u32 tpr, groups, cluster, slice, chunk_rows, chunks;     // softmax_split
+    float scale;
+    DropArgs drop;
+    u32 buckets, side, both, reach;              // the bias: see include/adacomp.h (adacomp_relpos)
+    uint16_t first[ADACOMP_MAX_BUCKETS];
+};
+
+// softmax.cu, softmax_back.cu
+int launch_softmax(SoftmaxArgs &a, u32 type, cudaStream_t st);
+int launch_softmax_back(SoftmaxArgs &a, u32 type, cudaStream_t st);
+void softmax_split(SoftmaxArgs &a);
+
+}  // namespace adacomp_impl

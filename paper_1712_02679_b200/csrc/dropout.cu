@@ -1,0 +1,83 @@
+// Dropout from a counter-based generator: y = keep ? x * factor : 0, the mask recomputed wherever it is needed and never
+// stored.  Its backward pass is the same map applied to dy.
+#include "block.h"
+
+namespace adacomp_impl {
+
+constexpr int kDropThreads = 256;
+constexpr int kDropPer = 4;         // groups of eight (WIDE) per thread
+
+// Rows that start on a vector boundary: the tensor is one line of groups of eight.
+template <u32 TYPE>
+__global__ void __launch_bounds__(kDropThreads)
+dropout_wide(const void *x, void *y, u32 row0, u32 n_groups, FastDiv per_row, DropArgs args)
+{
+    const Drop d = drop_begin(args);
+    const u32 g0 = blockIdx.x * (kDropThreads * kDropPer) + threadIdx.x;
+    const u64 at0 = (u64)row0 * per_row.d * 8u;
+    Vec8<TYPE> r[kDropPer];
+#pragma unroll
+    for (int i = 0; i < kDropPer; i++) {
+        const u32 g = g0 + i * kDropThreads;
+        if (g < n_groups) r[i] = load8<TYPE>(x, at0 + (u64)g * 8u);
+    }
+#pragma unroll
+    for (int i = 0; i < kDropPer; i++) {
+        const u32 g = g0 + i * kDropThreads;
+        if (g >= n_groups) break;
+        const u32 row = fast_div(g, per_row);
+        u32 w[4];
+        philox(d, g - row * per_row.d, row0 + row, w);
+        float v[8];
+        widen8<TYPE>(r[i], v);
+        drop_apply(d, w, v);
+        store8<TYPE>(y, at0 + (u64)g * 8u, narrow8<TYPE>(v));
+    }
+}
+
+// Any row length: a warp takes 256 columns of a row.
+template <u32 TYPE>
+__global__ void __launch_bounds__(kDropThreads)
+dropout_any(const void *x, void *y, u32 row0, u32 n_items, u32 cols, FastDiv per_row, DropArgs args)
+{
+    const Drop d = drop_begin(args);
+    const u32 lane = threadIdx.x & 31u, item = blockIdx.x * (kDropThreads / 32) + (threadIdx.x >> 5);
+    if (item >= n_items) return;
+    const u32 r = fast_div(item, per_row), k = item - r * per_row.d;
+    const u64 at = ((u64)row0 + r) * cols;
+    float v[8];
+    load_block<TYPE, false>(x, at, k, lane, 32, cols, 0.f, v);
+    u32 w[4];
+    drop_words<false>(d, row0 + r, 0, k, lane, 32, w);
+    drop_apply(d, w, v);
+    store_block<TYPE, false>(y, at, k, lane, 32, cols, v);
+}
+
+template <u32 TYPE>
+static void launch_type(const void *x, void *y, u64 rows, u32 cols, const DropArgs &drop, cudaStream_t st)
+{
+    const bool wide = cols % 8u == 0;
+    const u32 per_row = wide ? cols / 8u : (cols + 255u) / 256u;
+    const FastDiv f = make_fastdiv(per_row);
+    const u64 slice = 0x7fffffffu / per_row;         // rows a launch covers: items are numbered in 31 bits
+    for (u64 row0 = 0; row0 < rows; row0 += slice) {
+        const u32 items = (u32)((rows - row0 < slice ? rows - row0 : slice) * per_row);
+        if (wide) {
+            const u32 per_cta = kDropThreads * kDropPer;
+            dropout_wide<TYPE><<<(items - 1) / per_cta + 1, kDropThreads, 0, st>>>(x, y, (u32)row0, items, f, drop);
+        } else {
+            const u32 per_cta = kDropThreads / 32;
+            dropout_any<TYPE><<<(items - 1) / per_cta + 1, kDropThreads, 0, st>>>(x, y, (u32)row0, items, cols, f, drop);
+        }
+    }
+}
+
+int launch_dropout(const void *x, void *y, u64 rows, u32 cols, u32 type, const DropArgs &drop, cudaStream_t st)
+{
+    if (type == ADACOMP_TYPE_F32) launch_type<ADACOMP_TYPE_F32>(x, y, rows, cols, drop, st);
+    else if (type == ADACOMP_TYPE_BF16) launch_type<ADACOMP_TYPE_BF16>(x, y, rows, cols, drop, st);
+    else launch_type<ADACOMP_TYPE_F16>(x, y, rows, cols, drop, st);
+    return launched();
+}
+
+}  // namespace adacomp_impl

@@ -1,0 +1,175 @@
+// Layer norm, backward: the gradient of h (to the residual, and through dropout to x), and the weight's and bias's
+// gradients, which are sums over all rows.
+#include "norm.cuh"
+
+namespace adacomp_impl {
+
+// With xhat = (h - mean) rstd and g = dy weight:  dh = rstd (g - mean(g) - xhat mean(g xhat)) + dh_in.
+// A thread keeps its columns from row to row, so that dweight = sum dy xhat and dbias = sum dy grow in its registers; a
+// CTA leaves one line of each, and norm_back_sum adds the lines in their order.
+template <u32 TYPE, bool WIDE, int NV, bool DROP>
+__global__ void __launch_bounds__(kNormThreads) norm_backward(const NormArgs a)
+{
+    __shared__ float2 part[2][kNormThreads / 32];
+    __shared__ float2 peers[2][8];
+    __shared__ float merge[NV == 1 ? kNormThreads * 8 : 1];
+    const RowGroup rg(a.tpr);
+    const u32 rank = a.cluster > 1 ? cg::this_cluster().block_rank() : 0u;
+    if (a.cluster > 1) cg::this_cluster().sync();      // every CTA of the cluster runs before its memory is written
+    const u32 c0 = rank * a.slice, cols = min(a.slice, a.cols - c0);
+    const u32 first_warp = rg.g * rg.warps;
+    const void *wp = a.weight ? static_cast<const unsigned char *>(a.weight) + (u64)c0 * type_size(a.param_type) : nullptr;
+    float w[NV][8], dw[NV][8], db[NV][8];
+#pragma unroll
+    for (int k = 0; k < NV; k++) {
+        load_param<WIDE>(wp, a.param_type, k, rg.t, rg.tpr, cols, 1.f, w[k]);
+#pragma unroll
+        for (int e = 0; e < 8; e++) dw[k][e] = db[k][e] = 0.f;
+    }
+    Drop d;
+    if constexpr (DROP) d = drop_begin(a.drop);
+    const float inv_cols = 1.f / (float)a.cols;
+    const u32 set = blockIdx.x / a.cluster;
+    u32 parity = 0;
+    const u64 step = (u64)a.partials * a.groups;
+    for (u64 row = (u64)set * a.groups + rg.g; row < a.rows; row += step, parity ^= 1u) {
+        const u64 at = row * a.cols + c0;
+        float dy[NV][8], xh[NV][8];
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+            load_block<TYPE, WIDE>(a.dy, at, k, rg.t, rg.tpr, cols, 0.f, dy[k]);
+            load_block<TYPE, WIDE>(a.x, at, k, rg.t, rg.tpr, cols, mean, xh[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < NV; k++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                xh[k][e] = (xh[k][e] - mean) * rstd;
+                dw[k][e] += dy[k][e] * xh[k][e];
+                db[k][e] += dy[k][e];
+                dy[k][e] *= w[k][e];
+                s1 += dy[k][e];
+                s2 += dy[k][e] * xh[k][e];
+            }
+        s1 = warp_sum(s1);
+        s2 = warp_sum(s2);
+        if (rg.warps > 1) {
+            if (rg.lane == 0) part[parity][first_warp + rg.warp] = make_float2(s1, s2);
+            rg.sync();
+            const float2 p = rg.lane < rg.warps ? part[parity][first_warp + rg.lane] : make_float2(0.f, 0.f);
+            s1 = warp_sum(p.x);
+            s2 = warp_sum(p.y);
+        }
+        if (a.cluster > 1) {
+            cg::cluster_group cl = cg::this_cluster();
+            if (threadIdx.x < a.cluster) cl.map_shared_rank(&peers[parity][0], threadIdx.x)[rank] = make_float2(s1, s2);
+            cl.sync();
+            s1 = s2 = 0.f;
+            for (u32 i = 0; i < a.cluster; i++) {
+                s1 += peers[parity][i].x;
+                s2 += peers[parity][i].y;
+            }
+        }
+        s1 *= inv_cols;
+        s2 *= inv_cols;
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+#pragma unroll
+            for (int e = 0; e < 8; e++) dy[k][e] = rstd * (dy[k][e] - s1 - xh[k][e] * s2);
+            if (a.dh_in) {
+                load_block<TYPE, WIDE>(a.dh_in, at, k, rg.t, rg.tpr, cols, 0.f, xh[k]);
+#pragma unroll
+                for (int e = 0; e < 8; e++) dy[k][e] += xh[k][e];
+            }
+            if (a.dresidual) store_block<TYPE, WIDE>(a.dresidual, at, k, rg.t, rg.tpr, cols, dy[k]);
+            if constexpr (DROP) {
+                u32 bits[4];
+                drop_words<WIDE>(d, (u32)row, c0 >> 3, k, rg.t, rg.tpr, bits);
+                drop_apply(d, bits, dy[k]);
+            }
+            if (a.dx) store_block<TYPE, WIDE>(a.dx, at, k, rg.t, rg.tpr, cols, dy[k]);
+        }
+    }
+    if (!a.partial) return;
+    float *out = a.partial + (u64)set * 2 * a.cols + c0;
+#pragma unroll
+    for (int which = 0; which < 2; which++) {
+        float(&acc)[NV][8] = which ? db : dw;
+        if (NV == 1 && a.groups > 1) {          // rows of the CTA's groups, added in their order
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 8; e++) merge[e * kNormThreads + threadIdx.x] = acc[0][e];
+            __syncthreads();
+            if (rg.g == 0) {
+                for (u32 g = 1; g < a.groups; g++)
+#pragma unroll
+                    for (int e = 0; e < 8; e++) acc[0][e] += merge[e * kNormThreads + g * rg.tpr + rg.t];
+            }
+        }
+        if (rg.g == 0) {
+#pragma unroll
+            for (int k = 0; k < NV; k++)
+                if (WIDE) {
+                    const u32 c = column<true>(k, 0, rg.t, rg.tpr);
+                    if (c < cols) store8<ADACOMP_TYPE_F32>(out, (u64)which * a.cols + c, narrow8<ADACOMP_TYPE_F32>(acc[k]));
+                } else {
+                    store_block<ADACOMP_TYPE_F32, false>(out, (u64)which * a.cols, k, rg.t, rg.tpr, cols, acc[k]);
+                }
+        }
+    }
+}
+
+constexpr int kSumWarps = 16;
+
+// dweight (blockIdx.y = 0) and dbias: 32 columns per CTA, the CTAs' lines in a fixed order.
+__global__ void __launch_bounds__(32 * kSumWarps) norm_back_sum(const float *partial, u32 partials, u32 cols, void *dweight,
+                                                               void *dbias, u32 param_type)
+{
+    __shared__ float sums[kSumWarps][33];
+    void *out = blockIdx.y ? dbias : dweight;
+    if (!out) return;
+    const u32 lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, c = blockIdx.x * 32u + lane;
+    float s = 0.f;
+    if (c < cols)
+        for (u32 p = warp; p < partials; p += kSumWarps) s += partial[((u64)p * 2 + blockIdx.y) * cols + c];
+    sums[warp][lane] = s;
+    __syncthreads();
+    if (warp != 0 || c >= cols) return;
+    s = 0.f;
+    for (int i = 0; i < kSumWarps; i++) s += sums[i][lane];
+    if (param_type == ADACOMP_TYPE_F32) store1<ADACOMP_TYPE_F32>(out, c, s);
+    else if (param_type == ADACOMP_TYPE_BF16) store1<ADACOMP_TYPE_BF16>(out, c, s);
+    else store1<ADACOMP_TYPE_F16>(out, c, s);
+}
+
+template <u32 TYPE, bool WIDE, int NV> static void launch_drop(const NormArgs &a, cudaStream_t st)
+{
+    if (a.drop.threshold) launch_norm_kernel(norm_backward<TYPE, WIDE, NV, true>, a, a.partials, st);
+    else launch_norm_kernel(norm_backward<TYPE, WIDE, NV, false>, a, a.partials, st);
+}
+
+template <u32 TYPE> static void launch_type(const NormArgs &a, cudaStream_t st)
+{
+    const bool two = a.slice > a.tpr * 8u;
+    if (a.cols % 8u == 0) two ? launch_drop<TYPE, true, 2>(a, st) : launch_drop<TYPE, true, 1>(a, st);
+    else two ? launch_drop<TYPE, false, 2>(a, st) : launch_drop<TYPE, false, 1>(a, st);
+}
+
+int launch_norm_back(NormArgs &a, u32 type, cudaStream_t st)
+{
+    norm_split(a);
+    if (!a.dweight && !a.dbias) a.partial = nullptr;
+    if (a.rows) {
+        if (type == ADACOMP_TYPE_F32) launch_type<ADACOMP_TYPE_F32>(a, st);
+        else if (type == ADACOMP_TYPE_BF16) launch_type<ADACOMP_TYPE_BF16>(a, st);
+        else launch_type<ADACOMP_TYPE_F16>(a, st);
+    }
+    if (a.partial)
+        norm_back_sum<<<dim3((a.cols + 31u) / 32u, 2), 32 * kSumWarps, 0, st>>>(a.partial, a.rows ? a.partials : 0u, a.cols,
+                                                                              a.dweight, a.dbias, a.param_type);
+    return launched();
+}
+
+}  // namespace adacomp_impl
