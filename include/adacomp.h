@@ -532,7 +532,7 @@ int adacomp_debug_waits(uint64_t wait_cycles, uint32_t withhold_pack_tile, uint3
 #define ADACOMP_MAX_BUCKETS 128u      /* buckets of a relative position bias, both sides together */
 #define ADACOMP_MAX_DISTANCE 1024u    /* its max_distance */
 
-/* y = dropout(x) over [rows, cols]; the backward pass is the same call with dy for x. */
+/* y = dropout(x) over [rows, cols] (rows < 2^32, cols < 2^31); the backward pass is the same call with dy for x. */
 int adacomp_dropout(const void *x, void *y, uint64_t rows, uint32_t cols, uint32_t type, float p, const uint64_t *rng,
                     uint32_t site, void *stream);
 

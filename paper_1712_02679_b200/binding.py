@@ -50,6 +50,7 @@ ADACOMP_TYPE_F32, ADACOMP_TYPE_BF16, ADACOMP_TYPE_F16 = 0, 1, 2
 ADACOMP_MAX_NORM_COLS, ADACOMP_MAX_KEYS, ADACOMP_MAX_BUCKETS, ADACOMP_MAX_DISTANCE = 65536, 131072, 128, 1024
 _GRAD_DTYPES = {ADACOMP_GRAD_F32: torch.float32, ADACOMP_GRAD_BF16: torch.bfloat16, ADACOMP_GRAD_F16: torch.float16}
 
+_DTYPES = (torch.float32, torch.bfloat16, torch.float16)
 _TYPES = {torch.float32: ADACOMP_TYPE_F32, torch.bfloat16: ADACOMP_TYPE_BF16, torch.float16: ADACOMP_TYPE_F16}
 
 
@@ -193,6 +194,8 @@ def _dev_ptr(t: Optional[torch.Tensor], what: str, dtype=None) -> Optional[int]:
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
+        if torch.cuda.is_initialized():     # (the handle alone: building a Stream object costs 3 us a call)
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) or None
         return torch.cuda.current_stream().cuda_stream or None
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream or None
@@ -571,12 +574,14 @@ def _type_of(t: torch.Tensor, what: str) -> int:
 
 
 def _like(t: Optional[torch.Tensor], what: str, shape, dtype) -> Optional[int]:
-    """Pointer of a dense CUDA tensor of this shape and type (None: NULL)."""
+    """Pointer of a dense CUDA tensor of this shape (a torch.Size or a tuple) and type (None: NULL)."""
     if t is None:
         return None
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{what} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-    return _dev_ptr(t, what, dtype)
+    if t.is_cuda and t.dtype is dtype and t.is_contiguous():
+        return t.data_ptr()
+    return _dev_ptr(t, what, dtype)         # says what is wrong
 
 
 def _rng_ptr(rng: Optional[torch.Tensor]) -> Optional[int]:
@@ -594,31 +599,39 @@ def _rows_cols(x: torch.Tensor, what: str):
 def adacomp_dropout(x, y, p: float, rng, site: int = 0, stream=None) -> None:
     """y = dropout(x), rows being all dimensions but the last; the backward pass is the same call on dy."""
     rows, cols = _rows_cols(x, "x")
-    _check(lib().adacomp_dropout(_dev_ptr(x, "x"), _like(y, "y", x.shape, x.dtype), rows, cols, _type_of(x, "x"),
-                                 float(p), _rng_ptr(rng), int(site), _stream(stream)), "adacomp_dropout")
+    shape, dtype = x.shape, x.dtype
+    _check(lib().adacomp_dropout(_dev_ptr(x, "x"), _like(y, "y", shape, dtype), rows, cols, _type_of(x, "x"), p,
+                                 _rng_ptr(rng), site, _stream(stream)), "adacomp_dropout")
 
 
-def _norm_options(x, params, eps, p, rng, site):
-    rows, cols = _rows_cols(x, "x")
-    kinds = {t.dtype for t in params if t is not None}
-    if len(kinds) > 1:
-        raise ValueError("weight, bias and their gradients must have one dtype")
-    kind = _type_of(next(t for t in params if t is not None), "weight") if kinds else ADACOMP_TYPE_F32
-    return adacomp_norm_options(rows, cols, _type_of(x, "x"), kind, float(eps), float(p), int(site), _rng_ptr(rng))
+def _param_type(params, what: str) -> int:
+    kind = None
+    for t in params:
+        if t is not None:
+            if kind is not None and t.dtype is not kind:
+                raise ValueError(f"{what} must have one dtype")
+            kind = t.dtype
+    if kind is None:
+        return ADACOMP_TYPE_F32
+    if kind not in _TYPES:
+        raise ValueError(f"{what} must be float32, bfloat16 or float16")
+    return _TYPES[kind]
 
 
 def adacomp_layer_norm(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-5, residual=None, h_out=None,
                        p: float = 0.0, rng=None, site: int = 0, stream=None) -> None:
     """h = residual + dropout(x); y = layer_norm(h) * weight + bias over the last dimension.  mean, rstd: float32, one
     per row, for the backward call."""
-    opt = _norm_options(x, (weight, bias), eps, p, rng, site)
-    vec, stat = (opt.cols,), x.shape[:-1]
-    kind = weight.dtype if weight is not None else None
+    rows, cols = _rows_cols(x, "x")
+    kind = _param_type((weight, bias), "weight and bias")
+    opt = adacomp_norm_options(rows, cols, _type_of(x, "x"), kind, eps, p, site, _rng_ptr(rng))
+    shape, dtype, vec, f32 = x.shape, x.dtype, (cols,), torch.float32
+    stat = shape[:-1]
+    param = _DTYPES[kind]
     _check(lib().adacomp_layer_norm(
-        _dev_ptr(x, "x"), _like(residual, "residual", x.shape, x.dtype), _like(weight, "weight", vec, kind),
-        _like(bias, "bias", vec, bias.dtype if bias is not None else None), _like(h_out, "h_out", x.shape, x.dtype),
-        _like(y, "y", x.shape, x.dtype), _like(mean, "mean", stat, torch.float32), _like(rstd, "rstd", stat, torch.float32),
-        C.byref(opt), _stream(stream)), "adacomp_layer_norm")
+        _dev_ptr(x, "x"), _like(residual, "residual", shape, dtype), _like(weight, "weight", vec, param),
+        _like(bias, "bias", vec, param), _like(h_out, "h_out", shape, dtype), _like(y, "y", shape, dtype),
+        _like(mean, "mean", stat, f32), _like(rstd, "rstd", stat, f32), opt, _stream(stream)), "adacomp_layer_norm")
 
 
 def adacomp_layer_norm_workspace(rows: int, cols: int) -> int:
@@ -629,15 +642,18 @@ def adacomp_layer_norm_workspace(rows: int, cols: int) -> int:
 def adacomp_layer_norm_backward(dy, h, weight, mean, rstd, dx, dweight=None, dbias=None, workspace=None, dh_in=None,
                                 dresidual=None, p: float = 0.0, rng=None, site: int = 0, stream=None) -> None:
     """Gradients of adacomp_layer_norm; any output may be None.  dh_in: the gradient reaching h from elsewhere."""
-    opt = _norm_options(h, (weight, dweight, dbias), 0.0, p, rng, site)
-    vec, stat, n = (opt.cols,), h.shape[:-1], h.shape
-    param = next((t.dtype for t in (weight, dweight, dbias) if t is not None), None)
+    rows, cols = _rows_cols(h, "h")
+    kind = _param_type((weight, dweight, dbias), "weight, dweight and dbias")
+    opt = adacomp_norm_options(rows, cols, _type_of(h, "h"), kind, 0.0, p, site, _rng_ptr(rng))
+    shape, dtype, vec, f32 = h.shape, h.dtype, (cols,), torch.float32
+    stat = shape[:-1]
+    param = _DTYPES[kind]
     _check(lib().adacomp_layer_norm_backward(
-        _like(dy, "dy", n, h.dtype), _like(dh_in, "dh_in", n, h.dtype), _dev_ptr(h, "h"), _like(weight, "weight", vec, param),
-        _like(mean, "mean", stat, torch.float32), _like(rstd, "rstd", stat, torch.float32), _like(dx, "dx", n, h.dtype),
-        _like(dresidual, "dresidual", n, h.dtype), _like(dweight, "dweight", vec, param), _like(dbias, "dbias", vec, param),
-        _dev_ptr(workspace, "workspace", torch.uint8), workspace.numel() if workspace is not None else 0, C.byref(opt),
-        _stream(stream)), "adacomp_layer_norm_backward")
+        _like(dy, "dy", shape, dtype), _like(dh_in, "dh_in", shape, dtype), _dev_ptr(h, "h"),
+        _like(weight, "weight", vec, param), _like(mean, "mean", stat, f32), _like(rstd, "rstd", stat, f32),
+        _like(dx, "dx", shape, dtype), _like(dresidual, "dresidual", shape, dtype), _like(dweight, "dweight", vec, param),
+        _like(dbias, "dbias", vec, param), _dev_ptr(workspace, "workspace", torch.uint8),
+        workspace.numel() if workspace is not None else 0, opt, _stream(stream)), "adacomp_layer_norm_backward")
 
 
 def adacomp_relpos_plan(num_buckets: int, max_distance: int, bidirectional: bool = True) -> adacomp_relpos:
@@ -654,6 +670,8 @@ def _row_stride(t: torch.Tensor, what: str) -> Optional[int]:
         raise ValueError(f"{what} must be a CUDA tensor (no CPU path exists)")
     if t.dim() != 4:
         raise ValueError(f"{what} must be [batch, heads, queries, keys]")
+    if t.is_contiguous():
+        return t.shape[3] if t.numel() else None
     if t.numel() == 0:
         return None
     inner, ld = 1, None
@@ -672,19 +690,22 @@ def _row_stride(t: torch.Tensor, what: str) -> Optional[int]:
 def _softmax_call(scores, table, relpos, others, scale, causal, q_offset, key_len, p, rng, site):
     """Options of a softmax call and the table's pointer; `others`: (tensor, name) of the scores' shape."""
     ld = _row_stride(scores, "scores")
+    shape, dtype = scores.shape, scores.dtype
     for t, what in others:
-        if t.shape != scores.shape or t.dtype != scores.dtype:
+        if t.shape != shape or t.dtype is not dtype:
             raise ValueError(f"{what} must have the shape and dtype of scores")
         if _row_stride(t, what) != ld:
             raise ValueError(f"{what} must have the row stride of scores")
-    b, h, q, k = scores.shape
-    if table is not None and relpos is None:
-        raise ValueError("a bias table needs its buckets (adacomp_relpos_plan)")
-    tp = _like(table, "table", (relpos.num_buckets, h), torch.float32) if table is not None else None
-    opt = adacomp_softmax_options(b, h, q, k, ld if ld is not None else k, _type_of(scores, "scores"), float(scale),
-                                  int(bool(causal)), int(q_offset), _like(key_len, "key_len", (b,), torch.int32), float(p),
-                                  int(site), _rng_ptr(rng))
-    return opt, tp, C.byref(relpos) if table is not None else None
+    b, h, q, k = shape
+    tp = rel = None
+    if table is not None:
+        if relpos is None:
+            raise ValueError("a bias table needs its buckets (adacomp_relpos_plan)")
+        tp, rel = _like(table, "table", (relpos.num_buckets, h), torch.float32), relpos
+    opt = adacomp_softmax_options(b, h, q, k, ld if ld is not None else k, _type_of(scores, "scores"), scale,
+                                  1 if causal else 0, q_offset, _like(key_len, "key_len", (b,), torch.int32), p, site,
+                                  _rng_ptr(rng))
+    return opt, tp, rel
 
 
 def adacomp_bias_softmax(scores, table, relpos: Optional[adacomp_relpos], probs, lse=None, scale: float = 1.0,
@@ -693,7 +714,7 @@ def adacomp_bias_softmax(scores, table, relpos: Optional[adacomp_relpos], probs,
     """probs = dropout(softmax(scale * scores + bias)) over [batch, heads, queries, keys]; rows may be spaced apart."""
     opt, tp, rel = _softmax_call(scores, table, relpos, [(probs, "probs")], scale, causal, q_offset, key_len, p, rng, site)
     _check(lib().adacomp_bias_softmax(scores.data_ptr(), tp, rel, probs.data_ptr(),
-                                      _like(lse, "lse", scores.shape[:3], torch.float32), C.byref(opt), _stream(stream)),
+                                      _like(lse, "lse", scores.shape[:3], torch.float32), opt, _stream(stream)),
            "adacomp_bias_softmax")
 
 
@@ -711,5 +732,5 @@ def adacomp_bias_softmax_backward(dprobs, scores, table, relpos: Optional[adacom
     _check(lib().adacomp_bias_softmax_backward(
         dprobs.data_ptr(), scores.data_ptr(), tp, rel, _like(lse, "lse", scores.shape[:3], torch.float32),
         dscores.data_ptr(), _like(dtable, "dtable", table.shape if table is not None else (), torch.float32),
-        _dev_ptr(workspace, "workspace", torch.uint8), workspace.numel() if workspace is not None else 0, C.byref(opt),
+        _dev_ptr(workspace, "workspace", torch.uint8), workspace.numel() if workspace is not None else 0, opt,
         _stream(stream)), "adacomp_bias_softmax_backward")

@@ -102,7 +102,7 @@ int adacomp_dropout(const void *x, void *y, uint64_t rows, uint32_t cols, uint32
                     uint32_t site, void *stream)
 {
     if (type > ADACOMP_TYPE_F16) return ADACOMP_ERR_TYPE;
-    if (rows >= (1ull << 32)) return ADACOMP_ERR_SHAPE;
+    if (rows >= (1ull << 32) || cols >= (1u << 31)) return ADACOMP_ERR_SHAPE;
     DropArgs drop;
     if (!drop_args(p, rng, site, drop)) return ADACOMP_ERR_VALUE;
     if (rows == 0 || cols == 0) return ADACOMP_OK;

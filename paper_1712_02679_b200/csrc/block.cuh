@@ -100,71 +100,170 @@ template <u32 TYPE> __device__ inline void store1(void *base, u64 e, float v)
 // ---------------------------------------------------------------------------------
 // how a row's threads share its columns
 //
-// A row belongs to `tpr` threads (a multiple of 32); each holds blocks k = 0, 1, .. of eight elements.
-//   WIDE   rows start on a vector boundary (their length is a multiple of 8): block k of thread t is the eight
-//          neighbouring columns from 8 * (k * tpr + t) on, one 16-byte access (two for binary32)
-//   else   any length: element e of block k is column (8 k + e) * tpr + t, so that each access of a warp covers 32
-//          neighbouring elements wherever the row starts
+// A row belongs to `tpr` threads (whole warps); each holds NV blocks of eight neighbouring columns.  A warp's blocks lie
+// next to each other: block k of lane l of the row's warp w starts at column 8 * ((w * NV + k) * 32 + l).  So a block is
+// one group of the dropout generator, parameters are read by whole vectors, and neighbouring lanes hold neighbouring
+// columns.
+//
+// In memory a row may start anywhere (its length need not be a multiple of 8).  ALIGNED rows start on a 16-byte boundary.
+// Others start s elements behind one: a block then lies in two 16-byte chunks (three for binary32), which are loaded whole
+// and shifted; on the way out a lane joins its first elements with its neighbour's last ones into one whole chunk, and
+// only the ends of a warp's or a row's columns are stored element by element.  Chunks are loaded only if they hold an
+// element of the block, so no 16-byte granule without an element of the tensor is touched.
 // ---------------------------------------------------------------------------------
 
-template <bool WIDE> __device__ inline u32 column(u32 k, u32 e, u32 t, u32 tpr)
-{
-    return WIDE ? (k * tpr + t) * 8u + e : (k * 8u + e) * tpr + t;
-}
+template <int NV> __device__ inline u32 block_column(u32 k, u32 t) { return (((t >> 5) * NV + k) * 32u + (t & 31u)) * 8u; }
 
-// Elements of block k that lie before column `end`; the others are `fill` (WIDE reads whole vectors, which lie inside
-// the row because the distance between rows is a multiple of 8).
-template <u32 TYPE, bool WIDE>
-__device__ inline void load_block(const void *base, u64 row_at, u32 k, u32 t, u32 tpr, u32 end, float fill, float (&v)[8])
+template <u32 TYPE> __host__ __device__ constexpr u32 chunk_elems() { return 16u / type_size(TYPE); }
+
+// A block as loaded, not yet shifted (what a prefetch holds).
+template <u32 TYPE, bool ALIGNED> struct Raw { uint4 q[(TYPE == ADACOMP_TYPE_F32 ? 2 : 1) + (ALIGNED ? 0 : 1)]; };
+
+// The block from column c of the row at element row_at, as far as it lies before column `end`.
+template <u32 TYPE, bool ALIGNED>
+__device__ inline void fetch(Raw<TYPE, ALIGNED> &r, const void *base, u64 row_at, u32 c, u32 end)
 {
-    if constexpr (WIDE) {
-        const u32 c = column<true>(k, 0, t, tpr);
-        if (c < end) widen8<TYPE>(load8<TYPE>(base, row_at + c), v);
-        if (c + 8 > end) {
+    constexpr u32 per = chunk_elems<TYPE>();
+    const u32 s = ALIGNED ? 0u : (u32)row_at & (per - 1u);
+    const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const unsigned char *>(base) + (row_at + c - s) * type_size(TYPE));
+    constexpr int n = sizeof(r.q) / 16;
 #pragma unroll
-            for (int e = 0; e < 8; e++)
-                if (c + e >= end) v[e] = fill;
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-            const u32 c = column<false>(k, e, t, tpr);
-            v[e] = c < end ? load1<TYPE>(base, row_at + c) : fill;
-        }
+    for (int i = 0; i < n; i++) {
+        r.q[i] = make_uint4(0u, 0u, 0u, 0u);
+        // chunk i holds columns c - s + i * per and up (the first one: column c)
+        if (c + (i ? i * per - s : 0u) < end && (ALIGNED || i * per - s < 8u || i == 0)) r.q[i] = p[i];
     }
 }
 
-template <u32 TYPE, bool WIDE>
-__device__ inline void store_block(void *base, u64 row_at, u32 k, u32 t, u32 tpr, u32 cols, const float (&v)[8])
+// w[0..n) = in[shift .. shift + n) for a shift of 0..3 words (the same for the whole warp)
+template <int N, int M> __device__ inline void shift_words(const u32 (&in)[M], u32 shift, u32 (&out)[N])
 {
-    if constexpr (WIDE) {
-        const u32 c = column<true>(k, 0, t, tpr);
+    u32 x[N + 1];
+#pragma unroll
+    for (int i = 0; i <= N; i++) x[i] = (shift & 2u) ? (i + 2 < M ? in[i + 2] : 0u) : (i < M ? in[i] : 0u);
+#pragma unroll
+    for (int i = 0; i < N; i++) out[i] = (shift & 1u) ? x[i + 1] : x[i];
+}
+
+// The block's elements in binary32; columns from `end` on are `fill`.
+template <u32 TYPE, bool ALIGNED>
+__device__ inline void unpack(const Raw<TYPE, ALIGNED> &r, u64 row_at, u32 c, u32 end, float fill, float (&v)[8])
+{
+    Vec8<TYPE> whole;
+    if constexpr (ALIGNED) {
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(whole.q) / 16); i++) whole.q[i] = r.q[i];
+    } else {
+        const u32 s = (u32)row_at & (chunk_elems<TYPE>() - 1u);
+        u32 *out = reinterpret_cast<u32 *>(whole.q);
+        constexpr int n = sizeof(r.q) / 4;
+        u32 in[n];
+#pragma unroll
+        for (int i = 0; i < n / 4; i++) in[4 * i] = r.q[i].x, in[4 * i + 1] = r.q[i].y, in[4 * i + 2] = r.q[i].z, in[4 * i + 3] = r.q[i].w;
+        if constexpr (TYPE == ADACOMP_TYPE_F32) {
+            u32 y[8];
+            shift_words<8>(in, s, y);
+#pragma unroll
+            for (int i = 0; i < 8; i++) out[i] = y[i];
+        } else {
+            u32 y[5];
+            shift_words<5>(in, s >> 1, y);
+#pragma unroll
+            for (int i = 0; i < 4; i++) out[i] = __funnelshift_r(y[i], y[i + 1], (s & 1u) * 16u);
+        }
+    }
+    widen8<TYPE>(whole, v);
+    if (c + 8 > end) {
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            if (c + e >= end) v[e] = fill;
+    }
+}
+
+template <u32 TYPE, bool ALIGNED>
+__device__ inline void load_block(const void *base, u64 row_at, u32 c, u32 end, float fill, float (&v)[8])
+{
+    Raw<TYPE, ALIGNED> r;
+    fetch<TYPE, ALIGNED>(r, base, row_at, c, end);
+    unpack<TYPE, ALIGNED>(r, row_at, c, end, fill, v);
+}
+
+// Stores the block's columns before `cols`.  Unless ALIGNED, all lanes of the warp take part, with neighbouring blocks.
+template <u32 TYPE, bool ALIGNED>
+__device__ inline void store_block(void *base, u64 row_at, u32 c, u32 cols, const float (&v)[8])
+{
+    constexpr u32 per = chunk_elems<TYPE>();
+    const u32 s = ALIGNED ? 0u : (u32)row_at & (per - 1u);
+    if (ALIGNED || s == 0u) {
         if (c + 8 <= cols) {
             store8<TYPE>(base, row_at + c, narrow8<TYPE>(v));
-        } else {                // what lies behind the row's last column is not this tensor's
+        } else if (c < cols) {          // what lies behind the row's last column is not this row's
 #pragma unroll
             for (int e = 0; e < 8; e++)
                 if (c + e < cols) store1<TYPE>(base, row_at + c + e, v[e]);
         }
-    } else {
+        return;
+    }
+    const u32 lane = threadIdx.x & 31u;
+    const Vec8<TYPE> mine8 = narrow8<TYPE>(v);
+    const u32 *n = reinterpret_cast<const u32 *>(mine8.q);
+    uint4 *p = reinterpret_cast<uint4 *>(static_cast<unsigned char *>(base) + (row_at + c - s) * type_size(TYPE));
+    const bool first = lane > 0u && c + per - s <= cols;            // the chunk that starts with the neighbour's elements
+    const bool next = lane < 31u && c + 8u + per - s <= cols;       // the chunk the next lane completes with mine
+    if constexpr (TYPE == ADACOMP_TYPE_F32) {
+        u32 in[12], out[8];
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-            const u32 c = column<false>(k, e, t, tpr);
-            if (c < cols) store1<TYPE>(base, row_at + c, v[e]);
+        for (int i = 0; i < 4; i++) in[i] = __shfl_up_sync(kAllLanes, n[4 + i], 1);
+#pragma unroll
+        for (int i = 0; i < 8; i++) in[4 + i] = n[i];
+        shift_words<8>(in, 4u - s, out);
+        const bool second = c + 8u - s <= cols;
+        if (first) p[0] = make_uint4(out[0], out[1], out[2], out[3]);
+        if (second) p[1] = make_uint4(out[4], out[5], out[6], out[7]);
+        if (!(first && second && next)) {
+#pragma unroll
+            for (u32 e = 0; e < 8; e++)
+                if (c + e < cols && (e < 4u - s ? !first : e < 8u - s ? !second : !next)) store1<TYPE>(base, row_at + c + e, v[e]);
+        }
+    } else {
+        u32 in[8], y[5];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            in[i] = __shfl_up_sync(kAllLanes, n[i], 1);
+            in[4 + i] = n[i];
+        }
+        shift_words<5>(in, (8u - s) >> 1, y);
+        u32 out[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) out[i] = __funnelshift_r(y[i], y[i + 1], (s & 1u) * 16u);
+        if (first) p[0] = make_uint4(out[0], out[1], out[2], out[3]);
+        if (!(first && next)) {
+#pragma unroll
+            for (u32 e = 0; e < 8; e++)
+                if (c + e < cols && (e < 8u - s ? !first : !next)) store1<TYPE>(base, row_at + c + e, v[e]);
         }
     }
 }
 
-// A parameter vector (its type known at run time) in the same layout.
-template <bool WIDE>
-__device__ inline void load_param(const void *p, u32 type, u32 k, u32 t, u32 tpr, u32 cols, float fill, float (&v)[8])
+// A parameter vector (its type known at run time; it starts on a vector boundary).
+__device__ inline void load_param(const void *p, u32 type, u32 c, u32 cols, float fill, float (&v)[8])
 {
 #pragma unroll
     for (int e = 0; e < 8; e++) v[e] = fill;
-    if (!p) return;
-    if (type == ADACOMP_TYPE_F32) load_block<ADACOMP_TYPE_F32, WIDE>(p, 0, k, t, tpr, cols, fill, v);
-    else if (type == ADACOMP_TYPE_BF16) load_block<ADACOMP_TYPE_BF16, WIDE>(p, 0, k, t, tpr, cols, fill, v);
-    else load_block<ADACOMP_TYPE_F16, WIDE>(p, 0, k, t, tpr, cols, fill, v);
+    if (!p || c >= cols) return;
+    if (c + 8 > cols) {
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            if (c + e < cols)
+                v[e] = type == ADACOMP_TYPE_F32 ? load1<ADACOMP_TYPE_F32>(p, c + e)
+                       : type == ADACOMP_TYPE_BF16 ? load1<ADACOMP_TYPE_BF16>(p, c + e) : load1<ADACOMP_TYPE_F16>(p, c + e);
+    } else if (type == ADACOMP_TYPE_F32) {
+        widen8<ADACOMP_TYPE_F32>(load8<ADACOMP_TYPE_F32>(p, c), v);
+    } else if (type == ADACOMP_TYPE_BF16) {
+        widen8<ADACOMP_TYPE_BF16>(load8<ADACOMP_TYPE_BF16>(p, c), v);
+    } else {
+        widen8<ADACOMP_TYPE_F16>(load8<ADACOMP_TYPE_F16>(p, c), v);
+    }
 }
 
 // ---------------------------------------------------------------------------------
@@ -181,17 +280,20 @@ struct DropArgs {
 };
 
 struct Drop {
-    u32 k0, k1, step, site, threshold;
+    u32 k0, k1, step, site;
+    u32 threshold;           // shifted to the upper half
+    bool all;                // p = 1
     float factor;
 };
 
 __device__ inline Drop drop_begin(const DropArgs &a)
 {
     const u64 seed = a.rng[0], step = a.rng[1];
-    return {(u32)seed, (u32)(seed >> 32), (u32)step, a.site, a.threshold, a.factor};
+    return {(u32)seed, (u32)(seed >> 32), (u32)step, a.site, a.threshold == 65536u ? 0xffffffffu : a.threshold << 16, a.threshold == 65536u, a.factor};
 }
 
-__device__ inline void philox(const Drop &d, u32 group, u32 row, u32 (&out)[4])
+// The eight 16-bit numbers of a block: group `group` of row `row`.
+__device__ inline void drop_words(const Drop &d, u32 row, u32 group, u32 (&out)[4])
 {
     u32 c0 = group, c1 = row, c2 = d.step, c3 = d.site, k0 = d.k0, k1 = d.k1;
 #pragma unroll
@@ -204,54 +306,15 @@ __device__ inline void philox(const Drop &d, u32 group, u32 row, u32 (&out)[4])
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
     }
-    out[0] = c0, out[1] = c1, out[2] = c2, out[3] = c3;
+    // (p = 1: the threshold 2^32 - 1 drops every word but one, so those words are made 0)
+    out[0] = d.all ? 0u : c0, out[1] = d.all ? 0u : c1, out[2] = d.all ? 0u : c2, out[3] = d.all ? 0u : c3;
 }
 
-// The random words of block k of thread t.  In the WIDE layout a block is one group.  In the other a group's columns lie
-// in one octet of lanes: lane q of the octet generates the group of element q, and an 8 x 8 transposition of 16-bit
-// halves among the octet (three exchanges) hands every lane its element of each group.  All lanes take part.
-// `group0`: the group of the first column of the threads' share of the row.
-template <bool WIDE> __device__ inline void drop_words(const Drop &d, u32 row, u32 group0, u32 k, u32 t, u32 tpr, u32 (&w)[4])
-{
-    if constexpr (WIDE) {
-        philox(d, group0 + k * tpr + t, row, w);
-    } else {
-        const u32 q = t & 7u;
-        philox(d, group0 + (((k * 8u + q) * tpr + (t & ~7u)) >> 3), row, w);
-        {
-            const bool up = q & 4u;
-            const u32 r0 = __shfl_xor_sync(kAllLanes, up ? w[0] : w[2], 4);
-            const u32 r1 = __shfl_xor_sync(kAllLanes, up ? w[1] : w[3], 4);
-            if (up) w[0] = r0, w[1] = r1;
-            else w[2] = r0, w[3] = r1;
-        }
-        {
-            const bool up = q & 2u;
-            const u32 r0 = __shfl_xor_sync(kAllLanes, up ? w[0] : w[1], 2);
-            const u32 r1 = __shfl_xor_sync(kAllLanes, up ? w[2] : w[3], 2);
-            if (up) w[0] = r0, w[2] = r1;
-            else w[1] = r0, w[3] = r1;
-        }
-        {
-            const bool up = q & 1u;
-            const u32 s0 = up ? __byte_perm(w[0], w[1], 0x5410) : __byte_perm(w[0], w[1], 0x7632);
-            const u32 s1 = up ? __byte_perm(w[2], w[3], 0x5410) : __byte_perm(w[2], w[3], 0x7632);
-            const u32 r0 = __shfl_xor_sync(kAllLanes, s0, 1);
-            const u32 r1 = __shfl_xor_sync(kAllLanes, s1, 1);
-            if (up) {       // keep the high halves, the partner's high halves go below them
-                w[0] = __byte_perm(r0, w[0], 0x7610), w[1] = __byte_perm(r0, w[1], 0x7632);
-                w[2] = __byte_perm(r1, w[2], 0x7610), w[3] = __byte_perm(r1, w[3], 0x7632);
-            } else {        // keep the low halves, the partner's low halves go above them
-                w[0] = __byte_perm(w[0], r0, 0x5410), w[1] = __byte_perm(w[1], r0, 0x7610);
-                w[2] = __byte_perm(w[2], r1, 0x5410), w[3] = __byte_perm(w[3], r1, 0x7610);
-            }
-        }
-    }
-}
-
+// Element e of a block is dropped when its half of the words is below the threshold: for the high halves a comparison of
+// the whole word with threshold << 16 says the same.
 __device__ inline bool dropped(const Drop &d, const u32 (&w)[4], int e)
 {
-    return ((e & 1) ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu) < d.threshold;
+    return ((e & 1) ? w[e >> 1] : w[e >> 1] << 16) < d.threshold;
 }
 
 // v = dropout(v): selected, not multiplied, so that infinities and NaN in dropped places leave zeros.
@@ -272,21 +335,32 @@ __device__ inline float warp_sum(float v)
     return v;
 }
 
+// The warp's largest value; NaN is passed over.
 __device__ inline float warp_max(float v)
 {
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor_sync(kAllLanes, v, d));
+    float m;
+    asm volatile("redux.sync.max.f32 %0, %1, %2;" : "=f"(m) : "f"(v), "r"(kAllLanes));
+    return m;
+}
+
+// The sum of lanes 0 .. span - 1 (span: a power of two), in all of those lanes.
+__device__ inline float lanes_sum(float v, u32 span)
+{
+    for (u32 d = span >> 1; d > 0; d >>= 1) v += __shfl_xor_sync(kAllLanes, v, d);
     return v;
 }
 
 // The threads of one row: `tpr` neighbouring threads of a CTA.  Rows of up to one warp need no barrier, others meet at
 // named barrier 1 + g (at most 15 rows share a CTA then).
 struct RowGroup {
-    u32 g, t, tpr, warps, warp, lane;
+    u32 g, t, tpr, warps, warp, lane, first_warp;
+    u32 span;               // the number of warps, rounded up to a power of two
     __device__ explicit RowGroup(u32 threads_per_row)
-        : g(threadIdx.x / threads_per_row), t(threadIdx.x % threads_per_row), tpr(threads_per_row),
-          warps(threads_per_row >> 5), warp(t >> 5), lane(t & 31u)
+        : g(threadIdx.x / threads_per_row), t(threadIdx.x - g * threads_per_row), tpr(threads_per_row),
+          warps(threads_per_row >> 5), warp(t >> 5), lane(t & 31u), first_warp(g * warps),
+          span(1)
     {
+        while (span < warps) span *= 2;
     }
     __device__ void sync() const
     {

@@ -22,7 +22,8 @@ struct NormArgs {
     float *partial;                              // [partials][2][cols]: sums of each CTA's rows
     u64 rows;
     u32 cols, param_type;
-    u32 tpr, groups, cluster, slice, partials;   // norm_split: threads per row, rows per CTA, CTAs per row, columns per CTA
+    // norm_split: threads per row, blocks of eight per thread, rows per CTA, CTAs per row, columns per CTA
+    u32 tpr, per, groups, cluster, slice, partials;
     float eps;
     DropArgs drop;
 };
@@ -44,7 +45,8 @@ struct SoftmaxArgs {
     u64 ld;
     u32 batch, heads, q_len, k_len, causal;
     int q_offset;
-    u32 tpr, groups, cluster, slice, chunk_rows, chunks;     // softmax_split
+    // softmax_split: as above; rows a group of threads takes one after the other, and a CTA's chunks per head
+    u32 tpr, per, groups, cluster, slice, run, chunks;
     float scale;
     DropArgs drop;
     u32 buckets, side, both, reach;              // the bias: see include/adacomp.h (adacomp_relpos)

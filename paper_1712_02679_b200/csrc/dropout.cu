@@ -5,7 +5,8 @@
 namespace adacomp_impl {
 
 constexpr int kDropThreads = 256;
-constexpr int kDropPer = 4;         // groups of eight (WIDE) per thread
+constexpr int kDropPer = 4;         // blocks of eight per thread, rows on a vector boundary
+constexpr int kDropAnyPer = 2;      // the same for any rows
 
 // Rows that start on a vector boundary: the tensor is one line of groups of eight.
 template <u32 TYPE>
@@ -27,7 +28,7 @@ dropout_wide(const void *x, void *y, u32 row0, u32 n_groups, FastDiv per_row, Dr
         if (g >= n_groups) break;
         const u32 row = fast_div(g, per_row);
         u32 w[4];
-        philox(d, g - row * per_row.d, row0 + row, w);
+        drop_words(d, row0 + row, g - row * per_row.d, w);
         float v[8];
         widen8<TYPE>(r[i], v);
         drop_apply(d, w, v);
@@ -35,22 +36,34 @@ dropout_wide(const void *x, void *y, u32 row0, u32 n_groups, FastDiv per_row, Dr
     }
 }
 
-// Any row length: a warp takes 256 columns of a row.
+// Any row length: a warp takes 256 columns of a row at a time.
 template <u32 TYPE>
 __global__ void __launch_bounds__(kDropThreads)
 dropout_any(const void *x, void *y, u32 row0, u32 n_items, u32 cols, FastDiv per_row, DropArgs args)
 {
     const Drop d = drop_begin(args);
-    const u32 lane = threadIdx.x & 31u, item = blockIdx.x * (kDropThreads / 32) + (threadIdx.x >> 5);
-    if (item >= n_items) return;
-    const u32 r = fast_div(item, per_row), k = item - r * per_row.d;
-    const u64 at = ((u64)row0 + r) * cols;
-    float v[8];
-    load_block<TYPE, false>(x, at, k, lane, 32, cols, 0.f, v);
-    u32 w[4];
-    drop_words<false>(d, row0 + r, 0, k, lane, 32, w);
-    drop_apply(d, w, v);
-    store_block<TYPE, false>(y, at, k, lane, 32, cols, v);
+    const u32 lane = threadIdx.x & 31u;
+    const u32 item0 = blockIdx.x * (kDropThreads / 32 * kDropAnyPer) + (threadIdx.x >> 5);
+    Raw<TYPE, false> raw[kDropAnyPer];
+#pragma unroll
+    for (int i = 0; i < kDropAnyPer; i++) {
+        const u32 item = item0 + i * (kDropThreads / 32);
+        const u32 r = fast_div(item, per_row), c = ((item - r * per_row.d) * 32u + lane) * 8u;
+        if (item < n_items) fetch<TYPE, false>(raw[i], x, ((u64)row0 + r) * cols, c, cols);
+    }
+#pragma unroll
+    for (int i = 0; i < kDropAnyPer; i++) {
+        const u32 item = item0 + i * (kDropThreads / 32);
+        if (item >= n_items) break;
+        const u32 r = fast_div(item, per_row), c = ((item - r * per_row.d) * 32u + lane) * 8u;
+        const u64 at = ((u64)row0 + r) * cols;
+        float v[8];
+        unpack<TYPE, false>(raw[i], at, c, cols, 0.f, v);
+        u32 w[4];
+        drop_words(d, row0 + r, c >> 3, w);
+        drop_apply(d, w, v);
+        store_block<TYPE, false>(y, at, c, cols, v);
+    }
 }
 
 template <u32 TYPE>
@@ -66,7 +79,7 @@ static void launch_type(const void *x, void *y, u64 rows, u32 cols, const DropAr
             const u32 per_cta = kDropThreads * kDropPer;
             dropout_wide<TYPE><<<(items - 1) / per_cta + 1, kDropThreads, 0, st>>>(x, y, (u32)row0, items, f, drop);
         } else {
-            const u32 per_cta = kDropThreads / 32;
+            const u32 per_cta = kDropThreads / 32 * kDropAnyPer;
             dropout_any<TYPE><<<(items - 1) / per_cta + 1, kDropThreads, 0, st>>>(x, y, (u32)row0, items, cols, f, drop);
         }
     }

@@ -8,7 +8,6 @@ namespace adacomp_impl {
 namespace cg = cooperative_groups;
 
 constexpr int kNormThreads = 512;            // most threads of a CTA
-constexpr u32 kNormSlice = 8192;             // most columns of one CTA: 512 threads, two blocks of eight each
 
 // Launches `kernel` over `rows_at_once` sets of rows, `cluster` CTAs to a row.
 template <typename K> inline void launch_norm_kernel(K kernel, const NormArgs &a, u32 sets, cudaStream_t st)

@@ -7,7 +7,7 @@ namespace adacomp_impl {
 // With xhat = (h - mean) rstd and g = dy weight:  dh = rstd (g - mean(g) - xhat mean(g xhat)) + dh_in.
 // A thread keeps its columns from row to row, so that dweight = sum dy xhat and dbias = sum dy grow in its registers; a
 // CTA leaves one line of each, and norm_back_sum adds the lines in their order.
-template <u32 TYPE, bool WIDE, int NV, bool DROP>
+template <u32 TYPE, bool ALIGNED, int NV, bool DROP>
 __global__ void __launch_bounds__(kNormThreads) norm_backward(const NormArgs a)
 {
     __shared__ float2 part[2][kNormThreads / 32];
@@ -17,12 +17,11 @@ __global__ void __launch_bounds__(kNormThreads) norm_backward(const NormArgs a)
     const u32 rank = a.cluster > 1 ? cg::this_cluster().block_rank() : 0u;
     if (a.cluster > 1) cg::this_cluster().sync();      // every CTA of the cluster runs before its memory is written
     const u32 c0 = rank * a.slice, cols = min(a.slice, a.cols - c0);
-    const u32 first_warp = rg.g * rg.warps;
     const void *wp = a.weight ? static_cast<const unsigned char *>(a.weight) + (u64)c0 * type_size(a.param_type) : nullptr;
     float w[NV][8], dw[NV][8], db[NV][8];
 #pragma unroll
     for (int k = 0; k < NV; k++) {
-        load_param<WIDE>(wp, a.param_type, k, rg.t, rg.tpr, cols, 1.f, w[k]);
+        load_param(wp, a.param_type, block_column<NV>(k, rg.t), cols, 1.f, w[k]);
 #pragma unroll
         for (int e = 0; e < 8; e++) dw[k][e] = db[k][e] = 0.f;
     }
@@ -32,16 +31,34 @@ __global__ void __launch_bounds__(kNormThreads) norm_backward(const NormArgs a)
     const u32 set = blockIdx.x / a.cluster;
     u32 parity = 0;
     const u64 step = (u64)a.partials * a.groups;
-    for (u64 row = (u64)set * a.groups + rg.g; row < a.rows; row += step, parity ^= 1u) {
+    u64 row = (u64)set * a.groups + rg.g;
+    Raw<TYPE, ALIGNED> ry[NV], rh[NV], ri[NV];
+    float next_mean = 0.f, next_rstd = 0.f;
+    auto fetch_row = [&](u64 r) {
+        const u32 end = r < a.rows ? cols : 0u;
+        if (r < a.rows) next_mean = a.mean[r], next_rstd = a.rstd[r];
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+            const u32 c = block_column<NV>(k, rg.t);
+            fetch<TYPE, ALIGNED>(ry[k], a.dy, r * a.cols + c0, c, end);
+            fetch<TYPE, ALIGNED>(rh[k], a.x, r * a.cols + c0, c, end);
+            if (a.dh_in) fetch<TYPE, ALIGNED>(ri[k], a.dh_in, r * a.cols + c0, c, end);
+        }
+    };
+    fetch_row(row);
+    for (; row < a.rows; row += step, parity ^= 1u) {
         const u64 at = row * a.cols + c0;
-        float dy[NV][8], xh[NV][8];
-        const float mean = a.mean[row], rstd = a.rstd[row];
+        float dy[NV][8], xh[NV][8], in[NV][8];
+        const float mean = next_mean, rstd = next_rstd;
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; k++) {
-            load_block<TYPE, WIDE>(a.dy, at, k, rg.t, rg.tpr, cols, 0.f, dy[k]);
-            load_block<TYPE, WIDE>(a.x, at, k, rg.t, rg.tpr, cols, mean, xh[k]);
+            const u32 c = block_column<NV>(k, rg.t);
+            unpack<TYPE, ALIGNED>(ry[k], at, c, cols, 0.f, dy[k]);
+            unpack<TYPE, ALIGNED>(rh[k], at, c, cols, mean, xh[k]);
+            if (a.dh_in) unpack<TYPE, ALIGNED>(ri[k], at, c, cols, 0.f, in[k]);
         }
+        fetch_row(row + step);          // the next row is on its way while this one is worked on
 #pragma unroll
         for (int k = 0; k < NV; k++)
 #pragma unroll
@@ -56,11 +73,12 @@ __global__ void __launch_bounds__(kNormThreads) norm_backward(const NormArgs a)
         s1 = warp_sum(s1);
         s2 = warp_sum(s2);
         if (rg.warps > 1) {
-            if (rg.lane == 0) part[parity][first_warp + rg.warp] = make_float2(s1, s2);
+            if (rg.lane == 0) part[parity][rg.first_warp + rg.warp] = make_float2(s1, s2);
             rg.sync();
-            const float2 p = rg.lane < rg.warps ? part[parity][first_warp + rg.lane] : make_float2(0.f, 0.f);
-            s1 = warp_sum(p.x);
-            s2 = warp_sum(p.y);
+            const u32 i = rg.lane & (rg.span - 1u);         // every span of lanes adds all the warps' values
+            const float2 p = i < rg.warps ? part[parity][rg.first_warp + i] : make_float2(0.f, 0.f);
+            s1 = lanes_sum(p.x, rg.span);
+            s2 = lanes_sum(p.y, rg.span);
         }
         if (a.cluster > 1) {
             cg::cluster_group cl = cg::this_cluster();
@@ -79,21 +97,22 @@ __global__ void __launch_bounds__(kNormThreads) norm_backward(const NormArgs a)
 #pragma unroll
             for (int e = 0; e < 8; e++) dy[k][e] = rstd * (dy[k][e] - s1 - xh[k][e] * s2);
             if (a.dh_in) {
-                load_block<TYPE, WIDE>(a.dh_in, at, k, rg.t, rg.tpr, cols, 0.f, xh[k]);
 #pragma unroll
-                for (int e = 0; e < 8; e++) dy[k][e] += xh[k][e];
+                for (int e = 0; e < 8; e++) dy[k][e] += in[k][e];
             }
-            if (a.dresidual) store_block<TYPE, WIDE>(a.dresidual, at, k, rg.t, rg.tpr, cols, dy[k]);
+            const u32 c = block_column<NV>(k, rg.t);
+            if (a.dresidual) store_block<TYPE, ALIGNED>(a.dresidual, at, c, cols, dy[k]);
             if constexpr (DROP) {
                 u32 bits[4];
-                drop_words<WIDE>(d, (u32)row, c0 >> 3, k, rg.t, rg.tpr, bits);
+                drop_words(d, (u32)row, (c0 + c) >> 3, bits);
                 drop_apply(d, bits, dy[k]);
             }
-            if (a.dx) store_block<TYPE, WIDE>(a.dx, at, k, rg.t, rg.tpr, cols, dy[k]);
+            if (a.dx) store_block<TYPE, ALIGNED>(a.dx, at, c, cols, dy[k]);
         }
     }
     if (!a.partial) return;
-    float *out = a.partial + (u64)set * 2 * a.cols + c0;
+    float *out = a.partial;
+    const u64 line = (u64)set * 2 * a.cols + c0;
 #pragma unroll
     for (int which = 0; which < 2; which++) {
         float(&acc)[NV][8] = which ? db : dw;
@@ -111,12 +130,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_backward(const NormArgs a)
         if (rg.g == 0) {
 #pragma unroll
             for (int k = 0; k < NV; k++)
-                if (WIDE) {
-                    const u32 c = column<true>(k, 0, rg.t, rg.tpr);
-                    if (c < cols) store8<ADACOMP_TYPE_F32>(out, (u64)which * a.cols + c, narrow8<ADACOMP_TYPE_F32>(acc[k]));
-                } else {
-                    store_block<ADACOMP_TYPE_F32, false>(out, (u64)which * a.cols, k, rg.t, rg.tpr, cols, acc[k]);
-                }
+                store_block<ADACOMP_TYPE_F32, ALIGNED>(out, line + (u64)which * a.cols, block_column<NV>(k, rg.t), cols, acc[k]);
         }
     }
 }
@@ -144,15 +158,15 @@ __global__ void __launch_bounds__(32 * kSumWarps) norm_back_sum(const float *par
     else store1<ADACOMP_TYPE_F16>(out, c, s);
 }
 
-template <u32 TYPE, bool WIDE, int NV> static void launch_drop(const NormArgs &a, cudaStream_t st)
+template <u32 TYPE, bool ALIGNED, int NV> static void launch_drop(const NormArgs &a, cudaStream_t st)
 {
-    if (a.drop.threshold) launch_norm_kernel(norm_backward<TYPE, WIDE, NV, true>, a, a.partials, st);
-    else launch_norm_kernel(norm_backward<TYPE, WIDE, NV, false>, a, a.partials, st);
+    if (a.drop.threshold) launch_norm_kernel(norm_backward<TYPE, ALIGNED, NV, true>, a, a.partials, st);
+    else launch_norm_kernel(norm_backward<TYPE, ALIGNED, NV, false>, a, a.partials, st);
 }
 
 template <u32 TYPE> static void launch_type(const NormArgs &a, cudaStream_t st)
 {
-    const bool two = a.slice > a.tpr * 8u;
+    const bool two = a.per == 2u;
     if (a.cols % 8u == 0) two ? launch_drop<TYPE, true, 2>(a, st) : launch_drop<TYPE, true, 1>(a, st);
     else two ? launch_drop<TYPE, false, 2>(a, st) : launch_drop<TYPE, false, 1>(a, st);
 }

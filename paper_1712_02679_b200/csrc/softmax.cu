@@ -4,44 +4,58 @@
 
 namespace adacomp_impl {
 
-// How rows are shared, by the sizes alone: a warp per row up to 1024 keys (8 to 32 per lane), more warps up to 16384, a
-// cluster of CTAs beyond.  A group of threads takes `chunk_rows` rows of one head, so that it lays the head's bias out by
-// distance once.
+// How rows are shared, by the sizes alone: a warp per row up to 1024 keys (8, 16 or 32 of them per lane), up to 16 warps
+// with 16 per lane up to 8192, a cluster of up to 8 such CTAs up to 65536, with 32 per lane beyond.
 void softmax_split(SoftmaxArgs &a)
 {
+    const u32 blocks = (a.k_len + 7u) / 8u;
     a.cluster = 1;
-    while (a.k_len > a.cluster * kSoftSlice) a.cluster *= 2;
+    if (blocks <= 128u) {
+        a.per = blocks <= 32u ? 1u : blocks <= 64u ? 2u : 4u;
+        a.tpr = 32;
+        a.groups = kSoftShort / 32;
+    } else {
+        while (a.cluster < 8u && blocks > a.cluster * kSoftThreads * 2u) a.cluster *= 2;
+        a.per = blocks > 8u * kSoftThreads * 2u ? 4u : 2u;
+        const u32 each = (blocks + a.cluster - 1) / a.cluster;
+        a.tpr = ((each + a.per - 1) / a.per + 31u) & ~31u;
+        a.groups = a.cluster == 1 && a.tpr < kSoftShort ? kSoftShort / a.tpr : 1u;
+    }
     a.slice = a.cluster == 1 ? a.k_len : ((a.k_len + a.cluster - 1) / a.cluster + 7u) & ~7u;
-    const u32 blocks = (a.slice + 7u) / 8u;
-    a.tpr = blocks <= 128u ? 32u : ((blocks + 3u) / 4u + 31u) & ~31u;
-    a.groups = a.cluster == 1 && a.tpr < kSoftMinThreads ? kSoftMinThreads / a.tpr : 1u;
-    const u64 rows = (u64)a.batch * a.heads * a.q_len;
-    const u64 at_once = 2ull * kBlockSms * 1024 / ((u64)a.tpr * a.cluster);      // groups of two full waves
-    u64 chunk = rows / at_once;
-    chunk = chunk < 1 ? 1 : chunk > 64 ? 64 : chunk;
-    if (chunk > a.q_len) chunk = a.q_len;
-    a.chunk_rows = chunk < 1 ? 1u : (u32)chunk;
-    a.chunks = (a.q_len + a.chunk_rows - 1) / a.chunk_rows;
+    while (a.groups > 1 && a.groups > a.q_len) a.groups /= 2;
+    // runs long enough to lay out the head's bias rarely, short enough for four CTAs' worth of work per place on the GPU
+    const u64 rows = (u64)a.batch * a.heads * a.q_len, places = (u64)kBlockSms * 16 * 32 / a.tpr;
+    u64 run = rows / (places * 4);
+    run = run < 1 ? 1 : run > 16 ? 16 : run;
+    const u32 most = (a.q_len + a.groups - 1) / a.groups;
+    a.run = run < most ? (u32)run : most ? most : 1u;
+    a.chunks = (a.q_len + a.groups * a.run - 1) / (a.groups * a.run);
 }
 
 // A row stays in registers.  Each warp takes powers of two about its own maximum; the maxima and sums of the row's warps
 // are joined in one meeting, and what a warp holds is rescaled as it is stored.
-template <u32 TYPE, bool WIDE, int NV, bool DROP>
-__global__ void __launch_bounds__(kSoftThreads) softmax_forward(const SoftmaxArgs a)
+template <u32 TYPE, bool ALIGNED, int NV, bool DROP, int THREADS>
+__global__ void __launch_bounds__(THREADS) softmax_forward(const SoftmaxArgs a)
 {
-    extern __shared__ float tables[];
-    __shared__ float2 part[2][kSoftThreads / 32];
+    extern __shared__ float4 tables[];
+    __shared__ float2 part[2][THREADS / 32];
     __shared__ float2 peers[2][8];
+    float *bias = reinterpret_cast<float *>(tables);
     const RowGroup rg(a.tpr);
     const SoftmaxRows rows(a, rg);
-    if (!rows.any) return;
     if (a.cluster > 1) cg::this_cluster().sync();      // every CTA of the cluster runs before its memory is written
-    float *bias = tables + rg.g * table_floats(a.reach);
-    build_table(a, rg, rows.head, bias);
-    rg.sync();
+    Raw<TYPE, ALIGNED> raw[NV];
+    auto fetch_row = [&](u32 i) {
+        const u64 at = ((u64)rows.bh * a.q_len + i) * a.ld + rows.c0;
+        const u32 end = i < rows.i1 ? rows.end(a, i) : 0u;
+#pragma unroll
+        for (int k = 0; k < NV; k++) fetch<TYPE, ALIGNED>(raw[k], a.scores, at, block_column<NV>(k, rg.t), end);
+    };
+    fetch_row(rows.i0);
+    build_bias(a, rows.bh % a.heads, bias);
+    __syncthreads();
     Drop d;
     if constexpr (DROP) d = drop_begin(a.drop);
-    const u32 first_warp = rg.g * rg.warps;
     u32 parity = 0;
     for (u32 i = rows.i0; i < rows.i1; i++, parity ^= 1u) {
         const u64 row = (u64)rows.bh * a.q_len + i, at = row * a.ld + rows.c0;
@@ -50,33 +64,32 @@ __global__ void __launch_bounds__(kSoftThreads) softmax_forward(const SoftmaxArg
         float v[NV][8];
         float top = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < NV; k++) load_block<TYPE, WIDE>(a.scores, at, k, rg.t, rg.tpr, end, 0.f, v[k]);
-#pragma unroll
         for (int k = 0; k < NV; k++) {
-            to_logits<WIDE>(v[k], bias, (int)a.reach, a.scale, d0, k, rg.t, rg.tpr, end);
+            const u32 c = block_column<NV>(k, rg.t);
+            unpack<TYPE, ALIGNED>(raw[k], at, c, end, 0.f, v[k]);
+            add_bias(v[k], bias, (int)a.reach, a.scale, d0 + (int)c);
+            mask_from(v[k], c, end, -INFINITY);
 #pragma unroll
             for (int e = 0; e < 8; e++) top = fmaxf(top, v[k][e]);
         }
-        const float warp_top = warp_max(top);
-        const float about = warp_top == -INFINITY ? 0.f : warp_top;
-        const bool far = far_out(about);
-        const float about2 = about * kLog2e;
+        fetch_row(i + 1);               // the next row is on its way while this one is worked on
+        top = warp_max(top);
+        const float about = top == -INFINITY ? 0.f : top;
         float s = 0.f;
 #pragma unroll
-        for (int k = 0; k < NV; k++)
+        for (int k = 0; k < NV; k++) {
+            exp_about(v[k], about);
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                v[k][e] = exp_about(v[k][e], about, about2, far);
-                s += v[k][e];
-            }
+            for (int e = 0; e < 8; e++) s += v[k][e];
+        }
         s = warp_sum(s);
-        top = warp_top;
         if (rg.warps > 1) {
-            if (rg.lane == 0) part[parity][first_warp + rg.warp] = make_float2(warp_top, s);
+            if (rg.lane == 0) part[parity][rg.first_warp + rg.warp] = make_float2(top, s);
             rg.sync();
-            const float2 p = rg.lane < rg.warps ? part[parity][first_warp + rg.lane] : make_float2(-INFINITY, 0.f);
+            const u32 w = rg.lane & (rg.span - 1u);
+            const float2 p = w < rg.warps ? part[parity][rg.first_warp + w] : make_float2(-INFINITY, 0.f);
             top = warp_max(p.x);
-            s = warp_sum(p.y * exp2_fast((p.x - (top == -INFINITY ? 0.f : top)) * kLog2e));
+            s = lanes_sum(p.y * exp2_fast((p.x - (top == -INFINITY ? 0.f : top)) * kLog2e), rg.span);
         }
         if (a.cluster > 1) {
             cg::cluster_group cl = cg::this_cluster();
@@ -88,35 +101,43 @@ __global__ void __launch_bounds__(kSoftThreads) softmax_forward(const SoftmaxArg
                 s += peers[parity][j].y * exp2_fast((peers[parity][j].x - (top == -INFINITY ? 0.f : top)) * kLog2e);
         }
         // a row that keeps nothing has s = 0 and becomes zeros
-        const float f = s == 0.f ? 0.f : exp2_fast((about - (top == -INFINITY ? 0.f : top)) * kLog2e) / s;
+        float f = s == 0.f ? 0.f : exp2_fast((about - (top == -INFINITY ? 0.f : top)) * kLog2e) / s;
         if (a.lse && rg.t == 0 && rows.rank == 0) a.lse[row] = s == 0.f ? -INFINITY : top + log2f(s) * kLn2;
+        if constexpr (DROP) f *= d.factor;
 #pragma unroll
         for (int k = 0; k < NV; k++) {
-#pragma unroll
-            for (int e = 0; e < 8; e++) v[k][e] *= f;
+            const u32 c = block_column<NV>(k, rg.t);
             if constexpr (DROP) {
                 u32 bits[4];
-                drop_words<WIDE>(d, (u32)row, rows.c0 >> 3, k, rg.t, rg.tpr, bits);
-                drop_apply(d, bits, v[k]);
+                drop_words(d, (u32)row, (rows.c0 + c) >> 3, bits);
+#pragma unroll
+                for (int e = 0; e < 8; e++) v[k][e] = dropped(d, bits, e) ? 0.f : v[k][e] * f;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; e++) v[k][e] *= f;
             }
-            store_block<TYPE, WIDE>(a.probs, at, k, rg.t, rg.tpr, rows.cols, v[k]);
+            store_block<TYPE, ALIGNED>(a.probs, at, c, rows.cols, v[k]);
         }
     }
 }
 
-template <u32 TYPE, bool WIDE, int NV> static void launch_drop(const SoftmaxArgs &a, cudaStream_t st)
+template <u32 TYPE, bool ALIGNED, int NV, int THREADS> static void launch_drop(const SoftmaxArgs &a, cudaStream_t st)
 {
-    const size_t smem = (size_t)a.groups * table_floats(a.reach) * sizeof(float);
-    if (a.drop.threshold) launch_softmax_kernel(softmax_forward<TYPE, WIDE, NV, true>, a, smem, st);
-    else launch_softmax_kernel(softmax_forward<TYPE, WIDE, NV, false>, a, smem, st);
+    const size_t smem = bias_floats(a.reach) * sizeof(float);
+    if (a.drop.threshold) launch_softmax_kernel(softmax_forward<TYPE, ALIGNED, NV, true, THREADS>, a, smem, st);
+    else launch_softmax_kernel(softmax_forward<TYPE, ALIGNED, NV, false, THREADS>, a, smem, st);
 }
 
-template <u32 TYPE, bool WIDE> static void launch_blocks(const SoftmaxArgs &a, cudaStream_t st)
+template <u32 TYPE, bool ALIGNED> static void launch_blocks(const SoftmaxArgs &a, cudaStream_t st)
 {
-    const u32 per = (a.slice + a.tpr * 8u - 1) / (a.tpr * 8u);
-    if (per <= 1) launch_drop<TYPE, WIDE, 1>(a, st);
-    else if (per == 2) launch_drop<TYPE, WIDE, 2>(a, st);
-    else launch_drop<TYPE, WIDE, 4>(a, st);
+    if (a.tpr == 32) {
+        if (a.per == 1) launch_drop<TYPE, ALIGNED, 1, kSoftShort>(a, st);
+        else if (a.per == 2) launch_drop<TYPE, ALIGNED, 2, kSoftShort>(a, st);
+        else launch_drop<TYPE, ALIGNED, 4, kSoftShort>(a, st);
+    } else {
+        if (a.per == 2) launch_drop<TYPE, ALIGNED, 2, kSoftThreads>(a, st);
+        else launch_drop<TYPE, ALIGNED, 4, kSoftThreads>(a, st);
+    }
 }
 
 template <u32 TYPE> static void launch_type(const SoftmaxArgs &a, cudaStream_t st)

@@ -8,8 +8,7 @@ namespace adacomp_impl {
 namespace cg = cooperative_groups;
 
 constexpr int kSoftThreads = 512;            // most threads of a CTA
-constexpr u32 kSoftSlice = 16384;            // most columns of one CTA: 512 threads, four blocks of eight each
-constexpr u32 kSoftMinThreads = 128;         // short rows share a CTA of this many threads
+constexpr int kSoftShort = 128;              // threads of a CTA whose rows are one warp each
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // 2^x by the hardware's approximation (PTX ex2.approx: within 2 units in the last place); -inf gives 0.
@@ -20,19 +19,26 @@ __device__ inline float exp2_fast(float x)
     return y;
 }
 
-// e^(x - about), about not -inf.  The product with log2(e) is taken of the difference where that of `about` would
+// v = e^(v - about), about not -inf.  The product with log2(e) is taken of the difference where that of `about` would
 // overflow: rows of a type's lowest value (a mask added by the caller) keep their softmax.
-__device__ inline bool far_out(float about) { return !(fabsf(about) < 1e38f); }
-__device__ inline float exp_about(float x, float about, float about2, bool far)
+__device__ inline void exp_about(float (&v)[8], float about)
 {
-    return exp2_fast(far ? (x - about) * kLog2e : fmaf(x, kLog2e, -about2));
+    if (fabsf(about) < 1e38f) {
+        const float about2 = about * kLog2e;
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] = exp2_fast(fmaf(v[e], kLog2e, -about2));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] = exp2_fast((v[e] - about) * kLog2e);
+    }
 }
 
-// The bias by distance, for one head: entry d + reach for d = key - query in -reach .. reach, farther distances share the
-// end entries (their bucket is the last one of their side).  A thread of the WIDE layout reads eight neighbouring entries,
-// its neighbour the eight next to those: a gap after every eight entries puts those of 32 lanes into 32 banks.
-__device__ inline u32 padded(u32 i) { return i + (i >> 3); }
-__host__ __device__ inline u32 table_floats(u32 reach) { return (2 * reach + 1) + ((2 * reach + 1) >> 3) + 1; }
+// The bias by distance d = key - query, for one head: entry d + reach + 8, where distances beyond -reach and reach have
+// the value there (their bucket is the last one of their side) and eight entries on either side say so.  A block's eight
+// neighbouring distances start anywhere, so the line is kept four times, each shifted by one entry: two 16-byte reads of
+// the copy in which the first entry is aligned serve a block, with no test of where it lies.
+__host__ __device__ inline u32 bias_entries(u32 reach) { return (2 * reach + 16 + 1 + 3) & ~3u; }
+__host__ __device__ inline u32 bias_floats(u32 reach) { return 4 * bias_entries(reach); }
 
 __device__ inline u32 bucket_of(const SoftmaxArgs &a, int d)
 {
@@ -42,31 +48,54 @@ __device__ inline u32 bucket_of(const SoftmaxArgs &a, int d)
     return d > 0 && a.both ? b + a.side : b;
 }
 
-__device__ inline void build_table(const SoftmaxArgs &a, const RowGroup &rg, u32 head, float *bias)
+// Called by all threads of the CTA; the caller synchronises.
+__device__ inline void build_bias(const SoftmaxArgs &a, u32 head, float *bias)
 {
-    const int reach = (int)a.reach;
-    for (int i = (int)rg.t; i <= 2 * reach; i += (int)rg.tpr)
-        bias[padded(i)] = a.table ? a.table[(u64)bucket_of(a, i - reach) * a.heads + head] : 0.f;
+    const int reach = (int)a.reach, n = (int)bias_entries(a.reach);
+    for (int i = (int)threadIdx.x; i < n + 3; i += (int)blockDim.x) {
+        const int d = max(-reach, min(reach, i - 8 - reach));
+        const float v = a.table ? a.table[(u64)bucket_of(a, d) * a.heads + head] : 0.f;
+#pragma unroll
+        for (int s = 0; s < 4; s++)
+            if (i >= s && i - s < n) bias[s * n + i - s] = v;
+    }
 }
 
-// Which rows a group of threads works on, and where.
+// v: scores of a block whose first distance is d, replaced by logits.
+__device__ inline void add_bias(float (&v)[8], const float *bias, int reach, float scale, int d)
+{
+    const u32 i = (u32)(max(-reach - 8, min(reach, d)) + reach + 8), s = i & 3u;
+    const float4 *p = reinterpret_cast<const float4 *>(bias + s * bias_entries((u32)reach) + (i - s));
+    const float4 x = p[0], y = p[1];
+    v[0] = fmaf(v[0], scale, x.x), v[1] = fmaf(v[1], scale, x.y), v[2] = fmaf(v[2], scale, x.z), v[3] = fmaf(v[3], scale, x.w);
+    v[4] = fmaf(v[4], scale, y.x), v[5] = fmaf(v[5], scale, y.y), v[6] = fmaf(v[6], scale, y.z), v[7] = fmaf(v[7], scale, y.w);
+}
+
+__device__ inline void mask_from(float (&v)[8], u32 c, u32 end, float fill)
+{
+    if (c + 8 > end) {
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            if (c + e >= end) v[e] = fill;
+    }
+}
+
+// A CTA works on one head of one sequence, on `groups` runs of `run` rows that follow one another.
 struct SoftmaxRows {
-    u32 bh, head, i0, i1, rank, c0, cols;
+    u32 bh, chunk, i0, i1, rank, c0, cols;
     int bound;              // keys of this sequence
-    bool any;
     __device__ SoftmaxRows(const SoftmaxArgs &a, const RowGroup &rg)
     {
         rank = a.cluster > 1 ? cg::this_cluster().block_rank() : 0u;
-        const u64 id = (u64)(blockIdx.x / a.cluster) * a.groups + rg.g;
-        any = id < (u64)a.batch * a.heads * a.chunks;
-        bh = (u32)(id / a.chunks);
-        head = bh % a.heads;
-        i0 = (u32)(id % a.chunks) * a.chunk_rows;
-        i1 = min(i0 + a.chunk_rows, a.q_len);
+        const u32 id = blockIdx.x / a.cluster;
+        bh = id / a.chunks;
+        chunk = id - bh * a.chunks;
+        i0 = min((chunk * a.groups + rg.g) * a.run, a.q_len);
+        i1 = min(i0 + a.run, a.q_len);
         c0 = rank * a.slice;
         cols = c0 < a.k_len ? min(a.slice, a.k_len - c0) : 0u;
         bound = (int)a.k_len;
-        if (any && a.key_len) bound = max(0, min(bound, a.key_len[bh / a.heads]));
+        if (a.key_len) bound = max(0, min(bound, a.key_len[bh / a.heads]));
     }
     // one past the last kept column of row i, counted from this CTA's first
     __device__ u32 end(const SoftmaxArgs &a, u32 i) const
@@ -77,44 +106,11 @@ struct SoftmaxRows {
     }
 };
 
-// v: scores of block k, replaced by logits; columns from `end` on become -inf.  `d0`: distance key -
-// query of this CTA's first column.
-template <bool WIDE>
-__device__ inline void to_logits(float (&v)[8], const float *bias, int reach, float scale, int d0, u32 k, u32 t, u32 tpr, u32 end)
-{
-    if constexpr (WIDE) {
-        const u32 c = column<true>(k, 0, t, tpr);
-        const int d = d0 + (int)c;
-        if (d >= reach || d + 7 <= -reach) {
-            const float far = bias[padded(d >= reach ? 2 * reach : 0)];
-#pragma unroll
-            for (int e = 0; e < 8; e++) v[e] = fmaf(v[e], scale, far);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; e++)
-                v[e] = fmaf(v[e], scale, bias[padded(max(-reach, min(reach, d + e)) + reach)]);
-        }
-        if (c + 8 > end) {
-#pragma unroll
-            for (int e = 0; e < 8; e++)
-                if (c + e >= end) v[e] = -INFINITY;
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-            const u32 c = column<false>(k, e, t, tpr);
-            const int d = max(-reach, min(reach, d0 + (int)c));
-            v[e] = c < end ? fmaf(v[e], scale, bias[padded(d + reach)]) : -INFINITY;
-        }
-    }
-}
-
 template <typename K> inline void launch_softmax_kernel(K kernel, const SoftmaxArgs &a, size_t smem, cudaStream_t st)
 {
     if (smem > 48 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    const u64 sets = ((u64)a.batch * a.heads * a.chunks + a.groups - 1) / a.groups;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(sets * a.cluster));
+    cfg.gridDim = dim3((unsigned)((u64)a.batch * a.heads * a.chunks * a.cluster));
     cfg.blockDim = dim3(a.tpr * a.groups);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;

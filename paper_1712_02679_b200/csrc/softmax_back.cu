@@ -4,38 +4,68 @@
 namespace adacomp_impl {
 
 // P is formed again from the scores and the row's logarithm of the sum, dp = dropout'(dprobs), D = sum_j P dp, and
-// ds = P (dp - D).  The table's gradient adds ds by distance: within `reach` into a line of shared memory that belongs to
-// the row's threads (a row meets each distance once, and two rows are a meeting apart, so no addition needs to be atomic
-// and their order is fixed), beyond it into a register per side.  A group's sums leave by bucket, and softmax_back_sum
-// adds the groups' in their order.
-template <u32 TYPE, bool WIDE, int NV, bool DROP>
-__global__ void __launch_bounds__(kSoftThreads) softmax_backward(const SoftmaxArgs a)
+// ds = P (dp - D).
+//
+// The table's gradient needs the sums of ds along the diagonals.  A warp takes rows that follow one another, and from one
+// row to the next a distance moves on by one column: so a thread keeps one sum per column it holds and, with each row,
+// takes over its neighbour's, acc[e] = acc[e - 1] + ds[e] - the shift costs nothing but one exchange per block.  What
+// leaves the warp's last column, and at the end of the run all sums, goes by distance into the warp's own line of shared
+// memory (distances within `reach`) or into one of two registers (beyond it, where the bucket is the side's last).  No
+// addition is atomic, so the order is fixed.  The CTA's warps are added and leave as one sum per bucket;
+// softmax_back_sum adds the CTAs'.
+template <u32 TYPE, bool ALIGNED, int NV, bool DROP, int THREADS>
+__global__ void __launch_bounds__(THREADS) softmax_backward(const SoftmaxArgs a)
 {
-    extern __shared__ float tables[];
-    __shared__ float part[2][kSoftThreads / 32];
-    __shared__ float2 ends[kSoftThreads / 32];
+    extern __shared__ float4 tables[];
+    __shared__ float part[2][THREADS / 32];
+    __shared__ float2 ends[THREADS / 32];
     __shared__ float peers[2][8];
     const RowGroup rg(a.tpr);
     const SoftmaxRows rows(a, rg);
-    if (!rows.any) return;
     if (a.cluster > 1) cg::this_cluster().sync();      // every CTA of the cluster runs before its memory is written
     const int reach = (int)a.reach;
-    const u32 floats = table_floats(a.reach);
-    float *bias = tables + rg.g * 2 * floats, *sums = bias + floats;
-    build_table(a, rg, rows.head, bias);
-    for (u32 i = rg.t; i < floats; i += rg.tpr) sums[i] = 0.f;
-    rg.sync();
+    const u32 line = 2 * a.reach + 1, cta_warp = threadIdx.x >> 5, cta_warps = blockDim.x >> 5;
+    float *bias = reinterpret_cast<float *>(tables), *all_sums = bias + bias_floats(a.reach);
+    float *sums = all_sums + cta_warp * line;          // entry d + reach; those of -reach and reach stay 0
+    Raw<TYPE, ALIGNED> rs[NV], rd[NV];
+    float next_lse = -INFINITY;
+    auto fetch_row = [&](u32 i) {
+        const u64 row = (u64)rows.bh * a.q_len + i, at = row * a.ld + rows.c0;
+        const u32 end = i < rows.i1 ? rows.end(a, i) : 0u;
+        if (i < rows.i1) next_lse = a.lse[row];
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+            const u32 c = block_column<NV>(k, rg.t);
+            fetch<TYPE, ALIGNED>(rs[k], a.scores, at, c, end);
+            fetch<TYPE, ALIGNED>(rd[k], a.dprobs, at, c, end);
+        }
+    };
+    fetch_row(rows.i0);
+    build_bias(a, rows.bh % a.heads, bias);
+    for (u32 i = rg.lane; i < line; i += 32) sums[i] = 0.f;
+    __syncthreads();
     Drop d;
     if constexpr (DROP) d = drop_begin(a.drop);
-    const u32 first_warp = rg.g * rg.warps;
+    float acc[NV][8];
+#pragma unroll
+    for (int k = 0; k < NV; k++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) acc[k][e] = 0.f;
     float before = 0.f, behind = 0.f;        // distances <= -reach, >= reach
+    auto put = [&](int dist, float v) {
+        if (dist >= reach) behind += v;
+        else if (dist <= -reach) before += v;
+        else sums[dist + reach] += v;
+    };
+    const int last_col = (int)(rows.c0 + block_column<NV>(NV - 1, rg.t | 31u) + 7u);     // of the warp
     u32 parity = 0;
     auto row_sum = [&](float v) -> float {      // over the row's threads; all of them take part
         v = warp_sum(v);
         if (rg.warps > 1) {
-            if (rg.lane == 0) part[parity][first_warp + rg.warp] = v;
+            if (rg.lane == 0) part[parity][rg.first_warp + rg.warp] = v;
             rg.sync();
-            v = warp_sum(rg.lane < rg.warps ? part[parity][first_warp + rg.lane] : 0.f);
+            const u32 w = rg.lane & (rg.span - 1u);
+            v = lanes_sum(w < rg.warps ? part[parity][rg.first_warp + w] : 0.f, rg.span);
         }
         if (a.cluster > 1) {
             cg::cluster_group cl = cg::this_cluster();
@@ -49,35 +79,35 @@ __global__ void __launch_bounds__(kSoftThreads) softmax_backward(const SoftmaxAr
     };
     for (u32 i = rows.i0; i < rows.i1; i++) {
         const u64 row = (u64)rows.bh * a.q_len + i, at = row * a.ld + rows.c0;
-        const float lse = a.lse[row];
+        const float lse = next_lse;
         const u32 end = lse == -INFINITY ? 0u : rows.end(a, i);
-        const int d0 = (int)rows.c0 - ((int)i + a.q_offset);
-        // A sum's logarithm does not show beside a statistic this large (ulp 2^-9 and up): P is then normalised again.
-        // (A property of the row, so that all its threads meet in row_sum.)
-        const bool huge = lse != -INFINITY && fabsf(lse) > 16384.f, far = far_out(lse);
-        const float lse2 = lse * kLog2e;
+        const int pos = (int)i + a.q_offset;
         float p[NV][8], g[NV][8];
         float dot = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; k++) {
-            load_block<TYPE, WIDE>(a.scores, at, k, rg.t, rg.tpr, end, 0.f, p[k]);
-            load_block<TYPE, WIDE>(a.dprobs, at, k, rg.t, rg.tpr, end, 0.f, g[k]);
+            const u32 c = block_column<NV>(k, rg.t);
+            unpack<TYPE, ALIGNED>(rs[k], at, c, end, 0.f, p[k]);
+            unpack<TYPE, ALIGNED>(rd[k], at, c, end, 0.f, g[k]);
         }
+        fetch_row(i + 1);               // the next row is on its way while this one is worked on
 #pragma unroll
         for (int k = 0; k < NV; k++) {
-            to_logits<WIDE>(p[k], bias, reach, a.scale, d0, k, rg.t, rg.tpr, end);
+            const u32 c = block_column<NV>(k, rg.t);
+            add_bias(p[k], bias, reach, a.scale, (int)(rows.c0 + c) - pos);
             if constexpr (DROP) {
                 u32 bits[4];
-                drop_words<WIDE>(d, (u32)row, rows.c0 >> 3, k, rg.t, rg.tpr, bits);
+                drop_words(d, (u32)row, (rows.c0 + c) >> 3, bits);
                 drop_apply(d, bits, g[k]);
             }
+            exp_about(p[k], lse);
+            mask_from(p[k], c, end, 0.f);
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                p[k][e] = column<WIDE>(k, e, rg.t, rg.tpr) < end ? exp_about(p[k][e], lse, lse2, far) : 0.f;
-                dot = fmaf(p[k][e], g[k][e], dot);
-            }
+            for (int e = 0; e < 8; e++) dot = fmaf(p[k][e], g[k][e], dot);
         }
-        if (huge) {
+        // A sum's logarithm does not show beside a statistic this large (ulp 2^-9 and up): P is then normalised again.
+        // (A property of the row, so that all its threads meet in row_sum.)
+        if (lse != -INFINITY && fabsf(lse) > 16384.f) {
             float total = 0.f;
 #pragma unroll
             for (int k = 0; k < NV; k++)
@@ -92,71 +122,63 @@ __global__ void __launch_bounds__(kSoftThreads) softmax_backward(const SoftmaxAr
                 for (int e = 0; e < 8; e++) p[k][e] *= f;
         }
         dot = row_sum(dot);
+        float carry = 0.f;              // lane 0: the last sum of the block before
 #pragma unroll
         for (int k = 0; k < NV; k++) {
 #pragma unroll
             for (int e = 0; e < 8; e++) p[k][e] *= g[k][e] - dot;
             if (a.partial) {
-                if constexpr (WIDE) {
-                    const u32 c = column<true>(k, 0, rg.t, rg.tpr);
-                    const int dist = d0 + (int)c;
-                    if (c < end) {
-                        if (dist >= reach) {
+                const float from = __shfl_sync(kAllLanes, acc[k][7], (rg.lane + 31u) & 31u);
 #pragma unroll
-                            for (int e = 0; e < 8; e++) behind += p[k][e];
-                        } else if (dist + 7 <= -reach) {
-#pragma unroll
-                            for (int e = 0; e < 8; e++) before += p[k][e];
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 8; e++) {
-                                if (dist + e >= reach) behind += p[k][e];
-                                else if (dist + e <= -reach) before += p[k][e];
-                                else sums[padded(dist + e + reach)] += p[k][e];
-                            }
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; e++) {
-                        const u32 c = column<false>(k, e, rg.t, rg.tpr);
-                        const int dist = d0 + (int)c;
-                        if (c < end) {
-                            if (dist >= reach) behind += p[k][e];
-                            else if (dist <= -reach) before += p[k][e];
-                            else sums[padded(dist + reach)] += p[k][e];
-                        }
-                    }
-                }
+                for (int e = 7; e > 0; e--) acc[k][e] = acc[k][e - 1] + p[k][e];
+                acc[k][0] = (rg.lane ? from : carry) + p[k][0];
+                carry = from;
             }
 #pragma unroll
             for (int e = 0; e < 8; e++) p[k][e] *= a.scale;
-            store_block<TYPE, WIDE>(a.dscores, at, k, rg.t, rg.tpr, rows.cols, p[k]);
+            store_block<TYPE, ALIGNED>(a.dscores, at, block_column<NV>(k, rg.t), rows.cols, p[k]);
         }
-        if (rg.warps == 1) __syncwarp();         // the next row's additions follow this one's
+        if (a.partial && rg.lane == 0 && i > rows.i0) put(last_col - (pos - 1), carry);
     }
     if (!a.partial) return;
+    __syncwarp();
+    if (rows.i1 > rows.i0) {
+        const int pos = (int)(rows.i1 - 1u) + a.q_offset;
+#pragma unroll
+        for (int k = 0; k < NV; k++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                put((int)(rows.c0 + block_column<NV>(k, rg.t)) + e - pos, acc[k][e]);
+                __syncwarp();
+            }
+    }
     before = warp_sum(before);
     behind = warp_sum(behind);
-    if (rg.lane == 0) ends[first_warp + rg.warp] = make_float2(before, behind);
-    rg.sync();
-    before = behind = 0.f;
-    for (u32 w = 0; w < rg.warps; w++) {
-        before += ends[first_warp + w].x;
-        behind += ends[first_warp + w].y;
+    if (rg.lane == 0) ends[cta_warp] = make_float2(before, behind);
+    __syncthreads();
+    for (u32 i = threadIdx.x; i < line; i += blockDim.x) {
+        float s = 0.f;
+        for (u32 w = 0; w < cta_warps; w++) s += all_sums[w * line + i];
+        all_sums[i] = s;
     }
-    float *out = a.partial + (((u64)rows.bh * a.chunks + rows.i0 / a.chunk_rows) * a.cluster + rows.rank) * a.buckets;
-    for (u32 b = rg.t; b < a.buckets; b += rg.tpr) {
+    before = behind = 0.f;
+    for (u32 w = 0; w < cta_warps; w++) {
+        before += ends[w].x;
+        behind += ends[w].y;
+    }
+    __syncthreads();
+    float *out = a.partial + ((u64)blockIdx.x) * a.buckets;
+    for (u32 b = threadIdx.x; b < a.buckets; b += blockDim.x) {
         const bool ahead = b >= a.side;          // buckets of keys behind the query's position
         const u32 k = ahead ? b - a.side : b;
         const bool last = k + 1 == a.side;
         // distances first[k] .. first[k + 1] - 1 of this side; those from reach on are in the register sums
         const int from = a.first[k], to = last ? reach : (int)a.first[k + 1];
         float s = 0.f;
-        for (int n = ahead && from == 0 ? 1 : from; n < to; n++) s += sums[padded(ahead ? reach + n : reach - n)];
+        for (int n = ahead && from == 0 ? 1 : from; n < to; n++) s += all_sums[ahead ? reach + n : reach - n];
         if (last) s += ahead ? behind : before;
         if (b == 0 && !a.both) {                 // one-sided: every key behind the query's position counts as distance 0
-            for (int n = 1; n < reach; n++) s += sums[padded(reach + n)];
+            for (int n = 1; n < reach; n++) s += all_sums[reach + n];
             s += behind;
         }
         out[b] = s;
@@ -185,19 +207,23 @@ softmax_back_sum(const float *partial, float *dtable, u32 batch, u32 heads, u32 
     dtable[(u64)b * heads + head] = s;
 }
 
-template <u32 TYPE, bool WIDE, int NV> static void launch_drop(const SoftmaxArgs &a, cudaStream_t st)
+template <u32 TYPE, bool ALIGNED, int NV, int THREADS> static void launch_drop(const SoftmaxArgs &a, cudaStream_t st)
 {
-    const size_t smem = 2 * (size_t)a.groups * table_floats(a.reach) * sizeof(float);
-    if (a.drop.threshold) launch_softmax_kernel(softmax_backward<TYPE, WIDE, NV, true>, a, smem, st);
-    else launch_softmax_kernel(softmax_backward<TYPE, WIDE, NV, false>, a, smem, st);
+    const size_t smem = (bias_floats(a.reach) + (size_t)(a.tpr * a.groups / 32) * (2 * a.reach + 1)) * sizeof(float);
+    if (a.drop.threshold) launch_softmax_kernel(softmax_backward<TYPE, ALIGNED, NV, true, THREADS>, a, smem, st);
+    else launch_softmax_kernel(softmax_backward<TYPE, ALIGNED, NV, false, THREADS>, a, smem, st);
 }
 
-template <u32 TYPE, bool WIDE> static void launch_blocks(const SoftmaxArgs &a, cudaStream_t st)
+template <u32 TYPE, bool ALIGNED> static void launch_blocks(const SoftmaxArgs &a, cudaStream_t st)
 {
-    const u32 per = (a.slice + a.tpr * 8u - 1) / (a.tpr * 8u);
-    if (per <= 1) launch_drop<TYPE, WIDE, 1>(a, st);
-    else if (per == 2) launch_drop<TYPE, WIDE, 2>(a, st);
-    else launch_drop<TYPE, WIDE, 4>(a, st);
+    if (a.tpr == 32) {
+        if (a.per == 1) launch_drop<TYPE, ALIGNED, 1, kSoftShort>(a, st);
+        else if (a.per == 2) launch_drop<TYPE, ALIGNED, 2, kSoftShort>(a, st);
+        else launch_drop<TYPE, ALIGNED, 4, kSoftShort>(a, st);
+    } else {
+        if (a.per == 2) launch_drop<TYPE, ALIGNED, 2, kSoftThreads>(a, st);
+        else launch_drop<TYPE, ALIGNED, 4, kSoftThreads>(a, st);
+    }
 }
 
 template <u32 TYPE> static void launch_type(const SoftmaxArgs &a, cudaStream_t st)
