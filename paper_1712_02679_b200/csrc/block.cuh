@@ -119,7 +119,16 @@ template <u32 TYPE> __host__ __device__ constexpr u32 chunk_elems() { return 16u
 // A block as loaded, not yet shifted (what a prefetch holds).
 template <u32 TYPE, bool ALIGNED> struct Raw { uint4 q[(TYPE == ADACOMP_TYPE_F32 ? 2 : 1) + (ALIGNED ? 0 : 1)]; };
 
-// The block from column c of the row at element row_at, as far as it lies before column `end`.
+template <u32 TYPE, bool ALIGNED, int NV> __device__ inline void clear(Raw<TYPE, ALIGNED> (&r)[NV])
+{
+#pragma unroll
+    for (int k = 0; k < NV; k++)
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(r[k].q) / 16); i++) r[k].q[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+
+// The block from column c of the row at element row_at, as far as it lies before column `end`; chunks that are not loaded
+// keep what they held.
 template <u32 TYPE, bool ALIGNED>
 __device__ inline void fetch(Raw<TYPE, ALIGNED> &r, const void *base, u64 row_at, u32 c, u32 end)
 {
@@ -129,7 +138,6 @@ __device__ inline void fetch(Raw<TYPE, ALIGNED> &r, const void *base, u64 row_at
     constexpr int n = sizeof(r.q) / 16;
 #pragma unroll
     for (int i = 0; i < n; i++) {
-        r.q[i] = make_uint4(0u, 0u, 0u, 0u);
         // chunk i holds columns c - s + i * per and up (the first one: column c)
         if (c + (i ? i * per - s : 0u) < end && (ALIGNED || i * per - s < 8u || i == 0)) r.q[i] = p[i];
     }
@@ -145,9 +153,9 @@ template <int N, int M> __device__ inline void shift_words(const u32 (&in)[M], u
     for (int i = 0; i < N; i++) out[i] = (shift & 1u) ? x[i + 1] : x[i];
 }
 
-// The block's elements in binary32; columns from `end` on are `fill`.
+// The block's elements in binary32 (see mask_from for those behind the last one asked for).
 template <u32 TYPE, bool ALIGNED>
-__device__ inline void unpack(const Raw<TYPE, ALIGNED> &r, u64 row_at, u32 c, u32 end, float fill, float (&v)[8])
+__device__ inline void unpack(const Raw<TYPE, ALIGNED> &r, u64 row_at, float (&v)[8])
 {
     Vec8<TYPE> whole;
     if constexpr (ALIGNED) {
@@ -173,19 +181,16 @@ __device__ inline void unpack(const Raw<TYPE, ALIGNED> &r, u64 row_at, u32 c, u3
         }
     }
     widen8<TYPE>(whole, v);
+}
+
+// v: the block from column c; its elements from column `end` on become `fill`.
+__device__ inline void mask_from(float (&v)[8], u32 c, u32 end, float fill)
+{
     if (c + 8 > end) {
 #pragma unroll
         for (int e = 0; e < 8; e++)
             if (c + e >= end) v[e] = fill;
     }
-}
-
-template <u32 TYPE, bool ALIGNED>
-__device__ inline void load_block(const void *base, u64 row_at, u32 c, u32 end, float fill, float (&v)[8])
-{
-    Raw<TYPE, ALIGNED> r;
-    fetch<TYPE, ALIGNED>(r, base, row_at, c, end);
-    unpack<TYPE, ALIGNED>(r, row_at, c, end, fill, v);
 }
 
 // Stores the block's columns before `cols`.  Unless ALIGNED, all lanes of the warp take part, with neighbouring blocks.
@@ -281,40 +286,54 @@ struct DropArgs {
 
 struct Drop {
     u32 k0, k1, step, site;
-    u32 threshold;           // shifted to the upper half
-    bool all;                // p = 1
+    u32 last;                // threshold * 2^16 - 1
     float factor;
 };
 
+// (for thresholds above 0)
 __device__ inline Drop drop_begin(const DropArgs &a)
 {
     const u64 seed = a.rng[0], step = a.rng[1];
-    return {(u32)seed, (u32)(seed >> 32), (u32)step, a.site, a.threshold == 65536u ? 0xffffffffu : a.threshold << 16, a.threshold == 65536u, a.factor};
+    return {(u32)seed, (u32)(seed >> 32), (u32)step, a.site, (a.threshold << 16) - 1u, a.factor};
 }
 
-// The eight 16-bit numbers of a block: group `group` of row `row`.
-__device__ inline void drop_words(const Drop &d, u32 row, u32 group, u32 (&out)[4])
+// The eight 16-bit numbers of N blocks: group[i] of row[i].  The blocks go through the rounds together: they share the
+// additions to the key, and (in one row) what the first two rounds make of the counter's constant parts.
+template <int N> __device__ inline void drop_words(const Drop &d, const u32 (&row)[N], const u32 (&group)[N], u32 (&out)[N][4])
 {
-    u32 c0 = group, c1 = row, c2 = d.step, c3 = d.site, k0 = d.k0, k1 = d.k1;
+    u32 k0 = d.k0, k1 = d.k1;
+#pragma unroll
+    for (int i = 0; i < N; i++) out[i][0] = group[i], out[i][1] = row[i], out[i][2] = d.step, out[i][3] = d.site;
 #pragma unroll
     for (int r = 0; r < 10; r++) {
-        const u64 a = (u64)c0 * 0xD2511F53u, b = (u64)c2 * 0xCD9E8D57u;
-        c0 = (u32)(b >> 32) ^ c1 ^ k0;
-        c2 = (u32)(a >> 32) ^ c3 ^ k1;
-        c1 = (u32)b;
-        c3 = (u32)a;
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            u32(&c)[4] = out[i];
+            const u64 a = (u64)c[0] * 0xD2511F53u, b = (u64)c[2] * 0xCD9E8D57u;
+            c[0] = (u32)(b >> 32) ^ c[1] ^ k0;
+            c[2] = (u32)(a >> 32) ^ c[3] ^ k1;
+            c[1] = (u32)b;
+            c[3] = (u32)a;
+        }
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
     }
-    // (p = 1: the threshold 2^32 - 1 drops every word but one, so those words are made 0)
-    out[0] = d.all ? 0u : c0, out[1] = d.all ? 0u : c1, out[2] = d.all ? 0u : c2, out[3] = d.all ? 0u : c3;
 }
 
-// Element e of a block is dropped when its half of the words is below the threshold: for the high halves a comparison of
-// the whole word with threshold << 16 says the same.
+__device__ inline void drop_words(const Drop &d, u32 row, u32 group, u32 (&out)[4])
+{
+    const u32 rows[1] = {row}, groups[1] = {group};
+    u32 w[1][4];
+    drop_words<1>(d, rows, groups, w);
+#pragma unroll
+    for (int i = 0; i < 4; i++) out[i] = w[0][i];
+}
+
+// Whether element e of a block is dropped: its half of the words is below the threshold.  For the high halves a comparison
+// of the whole word with threshold * 2^16 - 1 says the same.
 __device__ inline bool dropped(const Drop &d, const u32 (&w)[4], int e)
 {
-    return ((e & 1) ? w[e >> 1] : w[e >> 1] << 16) < d.threshold;
+    return ((e & 1) ? w[e >> 1] : w[e >> 1] << 16) <= d.last;
 }
 
 // v = dropout(v): selected, not multiplied, so that infinities and NaN in dropped places leave zeros.
@@ -343,24 +362,35 @@ __device__ inline float warp_max(float v)
     return m;
 }
 
-// The sum of lanes 0 .. span - 1 (span: a power of two), in all of those lanes.
-__device__ inline float lanes_sum(float v, u32 span)
+// Two sums over the warp for little more than the price of one: the first step leaves a's terms in the lower half of the
+// lanes and b's in the upper half.  Returns sum(a) to lanes 0..15, sum(b) to lanes 16..31.
+__device__ inline float warp_two_sums(float a, float b, u32 lane)
 {
-    for (u32 d = span >> 1; d > 0; d >>= 1) v += __shfl_xor_sync(kAllLanes, v, d);
+    const bool up = lane & 16u;
+    float v = (up ? b : a) + __shfl_xor_sync(kAllLanes, up ? a : b, 16);
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) v += __shfl_xor_sync(kAllLanes, v, d);
     return v;
 }
 
-// The threads of one row: `tpr` neighbouring threads of a CTA.  Rows of up to one warp need no barrier, others meet at
+// The sum over each half of the warp.
+__device__ inline float half_sum(float v)
+{
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) v += __shfl_xor_sync(kAllLanes, v, d);
+    return v;
+}
+
+__device__ inline float from_lane(float v, int lane) { return __shfl_sync(kAllLanes, v, lane); }
+
+// The threads of one row: `tpr` neighbouring threads of a CTA, at most 16 warps.  Rows of up to one warp need no barrier, others meet at
 // named barrier 1 + g (at most 15 rows share a CTA then).
 struct RowGroup {
     u32 g, t, tpr, warps, warp, lane, first_warp;
-    u32 span;               // the number of warps, rounded up to a power of two
     __device__ explicit RowGroup(u32 threads_per_row)
         : g(threadIdx.x / threads_per_row), t(threadIdx.x - g * threads_per_row), tpr(threads_per_row),
-          warps(threads_per_row >> 5), warp(t >> 5), lane(t & 31u), first_warp(g * warps),
-          span(1)
+          warps(threads_per_row >> 5), warp(t >> 5), lane(t & 31u), first_warp(g * warps)
     {
-        while (span < warps) span *= 2;
     }
     __device__ void sync() const
     {

@@ -8,6 +8,26 @@ namespace adacomp_impl {
 // Dropout's threshold and factor of a probability; false: not a probability.
 bool drop_args(float p, const void *rng, uint32_t site, DropArgs &out);
 
+// A second kernel that adds up what a first one left may be set up while the first one ends: the first says so when its
+// threads have little left to do, the second waits for its results (programmatic dependent launch).
+__device__ inline void after_kernel_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ inline void wait_for_kernel_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <typename... P, typename... A>
+inline void launch_after(void (*kernel)(P...), dim3 grid, unsigned threads, cudaStream_t st, A... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 int launched();        // ADACOMP_OK, or ADACOMP_ERR_CUDA when the last launch failed
 
 // dropout.cu

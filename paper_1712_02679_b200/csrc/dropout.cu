@@ -22,17 +22,21 @@ dropout_wide(const void *x, void *y, u32 row0, u32 n_groups, FastDiv per_row, Dr
         const u32 g = g0 + i * kDropThreads;
         if (g < n_groups) r[i] = load8<TYPE>(x, at0 + (u64)g * 8u);
     }
+    u32 row[kDropPer], group[kDropPer], w[kDropPer][4];
+#pragma unroll
+    for (int i = 0; i < kDropPer; i++) {
+        const u32 g = g0 + i * kDropThreads, q = fast_div(g, per_row);
+        row[i] = row0 + q;
+        group[i] = g - q * per_row.d;
+    }
+    drop_words<kDropPer>(d, row, group, w);
 #pragma unroll
     for (int i = 0; i < kDropPer; i++) {
         const u32 g = g0 + i * kDropThreads;
-        if (g >= n_groups) break;
-        const u32 row = fast_div(g, per_row);
-        u32 w[4];
-        drop_words(d, row0 + row, g - row * per_row.d, w);
         float v[8];
         widen8<TYPE>(r[i], v);
-        drop_apply(d, w, v);
-        store8<TYPE>(y, at0 + (u64)g * 8u, narrow8<TYPE>(v));
+        drop_apply(d, w[i], v);
+        if (g < n_groups) store8<TYPE>(y, at0 + (u64)g * 8u, narrow8<TYPE>(v));
     }
 }
 
@@ -58,7 +62,7 @@ dropout_any(const void *x, void *y, u32 row0, u32 n_items, u32 cols, FastDiv per
         const u32 r = fast_div(item, per_row), c = ((item - r * per_row.d) * 32u + lane) * 8u;
         const u64 at = ((u64)row0 + r) * cols;
         float v[8];
-        unpack<TYPE, false>(raw[i], at, c, cols, 0.f, v);
+        unpack<TYPE, false>(raw[i], at, v);
         u32 w[4];
         drop_words(d, row0 + r, c >> 3, w);
         drop_apply(d, w, v);
@@ -87,6 +91,11 @@ static void launch_type(const void *x, void *y, u64 rows, u32 cols, const DropAr
 
 int launch_dropout(const void *x, void *y, u64 rows, u32 cols, u32 type, const DropArgs &drop, cudaStream_t st)
 {
+    if (drop.threshold == 0) {          // nothing is dropped
+        if (x == y) return ADACOMP_OK;
+        return cudaMemcpyAsync(y, x, rows * cols * type_size(type), cudaMemcpyDeviceToDevice, st) == cudaSuccess
+                   ? ADACOMP_OK : ADACOMP_ERR_CUDA;
+    }
     if (type == ADACOMP_TYPE_F32) launch_type<ADACOMP_TYPE_F32>(x, y, rows, cols, drop, st);
     else if (type == ADACOMP_TYPE_BF16) launch_type<ADACOMP_TYPE_BF16>(x, y, rows, cols, drop, st);
     else launch_type<ADACOMP_TYPE_F16>(x, y, rows, cols, drop, st);

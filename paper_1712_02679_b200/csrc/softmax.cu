@@ -2,6 +2,12 @@
 // scale, the causal and length masks and dropout, in one pass.
 #include "softmax.cuh"
 
+#ifndef SFB
+#define SFB 1
+#endif
+#ifndef ONEW
+#define ONEW 128u
+#endif
 namespace adacomp_impl {
 
 // How rows are shared, by the sizes alone: a warp per row up to 1024 keys (8, 16 or 32 of them per lane), up to 16 warps
@@ -10,7 +16,7 @@ void softmax_split(SoftmaxArgs &a)
 {
     const u32 blocks = (a.k_len + 7u) / 8u;
     a.cluster = 1;
-    if (blocks <= 128u) {
+    if (blocks <= ONEW) {
         a.per = blocks <= 32u ? 1u : blocks <= 64u ? 2u : 4u;
         a.tpr = 32;
         a.groups = kSoftShort / 32;
@@ -35,7 +41,7 @@ void softmax_split(SoftmaxArgs &a)
 // A row stays in registers.  Each warp takes powers of two about its own maximum; the maxima and sums of the row's warps
 // are joined in one meeting, and what a warp holds is rescaled as it is stored.
 template <u32 TYPE, bool ALIGNED, int NV, bool DROP, int THREADS>
-__global__ void __launch_bounds__(THREADS) softmax_forward(const SoftmaxArgs a)
+__global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SFB : 1) softmax_forward(const SoftmaxArgs a)
 {
     extern __shared__ float4 tables[];
     __shared__ float2 part[2][THREADS / 32];
@@ -45,6 +51,7 @@ __global__ void __launch_bounds__(THREADS) softmax_forward(const SoftmaxArgs a)
     const SoftmaxRows rows(a, rg);
     if (a.cluster > 1) cg::this_cluster().sync();      // every CTA of the cluster runs before its memory is written
     Raw<TYPE, ALIGNED> raw[NV];
+    clear(raw);
     auto fetch_row = [&](u32 i) {
         const u64 at = ((u64)rows.bh * a.q_len + i) * a.ld + rows.c0;
         const u32 end = i < rows.i1 ? rows.end(a, i) : 0u;
@@ -57,39 +64,37 @@ __global__ void __launch_bounds__(THREADS) softmax_forward(const SoftmaxArgs a)
     Drop d;
     if constexpr (DROP) d = drop_begin(a.drop);
     u32 parity = 0;
+#pragma unroll 1
     for (u32 i = rows.i0; i < rows.i1; i++, parity ^= 1u) {
         const u64 row = (u64)rows.bh * a.q_len + i, at = row * a.ld + rows.c0;
         const u32 end = rows.end(a, i);
         const int d0 = (int)rows.c0 - ((int)i + a.q_offset);
         float v[NV][8];
-        float top = -INFINITY;
+        float top = -INFINITY, top2 = -INFINITY;
 #pragma unroll
         for (int k = 0; k < NV; k++) {
             const u32 c = block_column<NV>(k, rg.t);
-            unpack<TYPE, ALIGNED>(raw[k], at, c, end, 0.f, v[k]);
+            unpack<TYPE, ALIGNED>(raw[k], at, v[k]);
             add_bias(v[k], bias, (int)a.reach, a.scale, d0 + (int)c);
             mask_from(v[k], c, end, -INFINITY);
 #pragma unroll
-            for (int e = 0; e < 8; e++) top = fmaxf(top, v[k][e]);
+            for (int e = 0; e < 8; e += 2) top = fmaxf(top, v[k][e]), top2 = fmaxf(top2, v[k][e + 1]);
         }
         fetch_row(i + 1);               // the next row is on its way while this one is worked on
-        top = warp_max(top);
+        top = warp_max(fmaxf(top, top2));
         const float about = top == -INFINITY ? 0.f : top;
+        exp_about<NV>(v, about);
         float s = 0.f;
 #pragma unroll
-        for (int k = 0; k < NV; k++) {
-            exp_about(v[k], about);
-#pragma unroll
-            for (int e = 0; e < 8; e++) s += v[k][e];
-        }
+        for (int k = 0; k < NV; k++) s += ((v[k][0] + v[k][1]) + (v[k][2] + v[k][3])) + ((v[k][4] + v[k][5]) + (v[k][6] + v[k][7]));
         s = warp_sum(s);
         if (rg.warps > 1) {
             if (rg.lane == 0) part[parity][rg.first_warp + rg.warp] = make_float2(top, s);
             rg.sync();
-            const u32 w = rg.lane & (rg.span - 1u);
+            const u32 w = rg.lane & 15u;
             const float2 p = w < rg.warps ? part[parity][rg.first_warp + w] : make_float2(-INFINITY, 0.f);
             top = warp_max(p.x);
-            s = lanes_sum(p.y * exp2_fast((p.x - (top == -INFINITY ? 0.f : top)) * kLog2e), rg.span);
+            s = half_sum(p.y * exp2_fast((p.x - (top == -INFINITY ? 0.f : top)) * kLog2e));
         }
         if (a.cluster > 1) {
             cg::cluster_group cl = cg::this_cluster();
@@ -101,23 +106,30 @@ __global__ void __launch_bounds__(THREADS) softmax_forward(const SoftmaxArgs a)
                 s += peers[parity][j].y * exp2_fast((peers[parity][j].x - (top == -INFINITY ? 0.f : top)) * kLog2e);
         }
         // a row that keeps nothing has s = 0 and becomes zeros
-        float f = s == 0.f ? 0.f : exp2_fast((about - (top == -INFINITY ? 0.f : top)) * kLog2e) / s;
-        if (a.lse && rg.t == 0 && rows.rank == 0) a.lse[row] = s == 0.f ? -INFINITY : top + log2f(s) * kLn2;
+        float f = s == 0.f ? 0.f : exp2_fast((about - (top == -INFINITY ? 0.f : top)) * kLog2e) * __fdividef(1.f, s);
+        if (a.lse && rg.t == 0 && rows.rank == 0) a.lse[row] = s == 0.f ? -INFINITY : fmaf(__log2f(s), kLn2, top);
         if constexpr (DROP) f *= d.factor;
+        if constexpr (DROP) {
+            constexpr int N = NV < 2 ? 1 : 2;       // blocks that draw together
 #pragma unroll
-        for (int k = 0; k < NV; k++) {
-            const u32 c = block_column<NV>(k, rg.t);
-            if constexpr (DROP) {
-                u32 bits[4];
-                drop_words(d, (u32)row, (rows.c0 + c) >> 3, bits);
+            for (int k0 = 0; k0 < NV; k0 += N) {
+                u32 rws[N], groups[N], bits[N][4];
 #pragma unroll
-                for (int e = 0; e < 8; e++) v[k][e] = dropped(d, bits, e) ? 0.f : v[k][e] * f;
-            } else {
+                for (int k = 0; k < N; k++) rws[k] = (u32)row, groups[k] = (rows.c0 + block_column<NV>(k0 + k, rg.t)) >> 3;
+                drop_words<N>(d, rws, groups, bits);
+#pragma unroll
+                for (int k = 0; k < N; k++)
+#pragma unroll
+                    for (int e = 0; e < 8; e++) v[k0 + k][e] = dropped(d, bits[k], e) ? 0.f : v[k0 + k][e] * f;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < NV; k++)
 #pragma unroll
                 for (int e = 0; e < 8; e++) v[k][e] *= f;
-            }
-            store_block<TYPE, ALIGNED>(a.probs, at, c, rows.cols, v[k]);
         }
+#pragma unroll
+        for (int k = 0; k < NV; k++) store_block<TYPE, ALIGNED>(a.probs, at, block_column<NV>(k, rg.t), rows.cols, v[k]);
     }
 }
 

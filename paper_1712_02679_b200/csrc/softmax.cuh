@@ -21,15 +21,19 @@ __device__ inline float exp2_fast(float x)
 
 // v = e^(v - about), about not -inf.  The product with log2(e) is taken of the difference where that of `about` would
 // overflow: rows of a type's lowest value (a mask added by the caller) keep their softmax.
-__device__ inline void exp_about(float (&v)[8], float about)
+template <int NV> __device__ inline void exp_about(float (&v)[NV][8], float about)
 {
     if (fabsf(about) < 1e38f) {
         const float about2 = about * kLog2e;
 #pragma unroll
-        for (int e = 0; e < 8; e++) v[e] = exp2_fast(fmaf(v[e], kLog2e, -about2));
+        for (int k = 0; k < NV; k++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[k][e] = exp2_fast(fmaf(v[k][e], kLog2e, -about2));
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; e++) v[e] = exp2_fast((v[e] - about) * kLog2e);
+        for (int k = 0; k < NV; k++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[k][e] = exp2_fast((v[k][e] - about) * kLog2e);
     }
 }
 
@@ -69,15 +73,6 @@ __device__ inline void add_bias(float (&v)[8], const float *bias, int reach, flo
     const float4 x = p[0], y = p[1];
     v[0] = fmaf(v[0], scale, x.x), v[1] = fmaf(v[1], scale, x.y), v[2] = fmaf(v[2], scale, x.z), v[3] = fmaf(v[3], scale, x.w);
     v[4] = fmaf(v[4], scale, y.x), v[5] = fmaf(v[5], scale, y.y), v[6] = fmaf(v[6], scale, y.z), v[7] = fmaf(v[7], scale, y.w);
-}
-
-__device__ inline void mask_from(float (&v)[8], u32 c, u32 end, float fill)
-{
-    if (c + 8 > end) {
-#pragma unroll
-        for (int e = 0; e < 8; e++)
-            if (c + e >= end) v[e] = fill;
-    }
 }
 
 // A CTA works on one head of one sequence, on `groups` runs of `run` rows that follow one another.

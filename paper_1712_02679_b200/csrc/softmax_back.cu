@@ -1,6 +1,9 @@
 // The biased softmax's backward pass: the scores' gradient and the bias table's.
 #include "softmax.cuh"
 
+#ifndef SBB
+#define SBB 1
+#endif
 namespace adacomp_impl {
 
 // P is formed again from the scores and the row's logarithm of the sum, dp = dropout'(dprobs), D = sum_j P dp, and
@@ -14,7 +17,7 @@ namespace adacomp_impl {
 // addition is atomic, so the order is fixed.  The CTA's warps are added and leave as one sum per bucket;
 // softmax_back_sum adds the CTAs'.
 template <u32 TYPE, bool ALIGNED, int NV, bool DROP, int THREADS>
-__global__ void __launch_bounds__(THREADS) softmax_backward(const SoftmaxArgs a)
+__global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SBB : 1) softmax_backward(const SoftmaxArgs a)
 {
     extern __shared__ float4 tables[];
     __shared__ float part[2][THREADS / 32];
@@ -28,6 +31,8 @@ __global__ void __launch_bounds__(THREADS) softmax_backward(const SoftmaxArgs a)
     float *bias = reinterpret_cast<float *>(tables), *all_sums = bias + bias_floats(a.reach);
     float *sums = all_sums + cta_warp * line;          // entry d + reach; those of -reach and reach stay 0
     Raw<TYPE, ALIGNED> rs[NV], rd[NV];
+    clear(rs);
+    clear(rd);
     float next_lse = -INFINITY;
     auto fetch_row = [&](u32 i) {
         const u64 row = (u64)rows.bh * a.q_len + i, at = row * a.ld + rows.c0;
@@ -64,8 +69,8 @@ __global__ void __launch_bounds__(THREADS) softmax_backward(const SoftmaxArgs a)
         if (rg.warps > 1) {
             if (rg.lane == 0) part[parity][rg.first_warp + rg.warp] = v;
             rg.sync();
-            const u32 w = rg.lane & (rg.span - 1u);
-            v = lanes_sum(w < rg.warps ? part[parity][rg.first_warp + w] : 0.f, rg.span);
+            const u32 w = rg.lane & 15u;
+            v = half_sum(w < rg.warps ? part[parity][rg.first_warp + w] : 0.f);
         }
         if (a.cluster > 1) {
             cg::cluster_group cl = cg::this_cluster();
@@ -77,34 +82,47 @@ __global__ void __launch_bounds__(THREADS) softmax_backward(const SoftmaxArgs a)
         parity ^= 1u;
         return v;
     };
+#pragma unroll 1
     for (u32 i = rows.i0; i < rows.i1; i++) {
         const u64 row = (u64)rows.bh * a.q_len + i, at = row * a.ld + rows.c0;
         const float lse = next_lse;
         const u32 end = lse == -INFINITY ? 0u : rows.end(a, i);
         const int pos = (int)i + a.q_offset;
         float p[NV][8], g[NV][8];
-        float dot = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; k++) {
             const u32 c = block_column<NV>(k, rg.t);
-            unpack<TYPE, ALIGNED>(rs[k], at, c, end, 0.f, p[k]);
-            unpack<TYPE, ALIGNED>(rd[k], at, c, end, 0.f, g[k]);
+            unpack<TYPE, ALIGNED>(rs[k], at, p[k]);
+            unpack<TYPE, ALIGNED>(rd[k], at, g[k]);
+            add_bias(p[k], bias, reach, a.scale, (int)(rows.c0 + c) - pos);
+            mask_from(p[k], c, end, -INFINITY);
+            mask_from(g[k], c, end, 0.f);
         }
         fetch_row(i + 1);               // the next row is on its way while this one is worked on
+        if constexpr (DROP) {           // (the factor comes with dot, and where dp is used)
+            constexpr int N = NV < 2 ? 1 : 2;       // blocks that draw together
 #pragma unroll
-        for (int k = 0; k < NV; k++) {
-            const u32 c = block_column<NV>(k, rg.t);
-            add_bias(p[k], bias, reach, a.scale, (int)(rows.c0 + c) - pos);
-            if constexpr (DROP) {
-                u32 bits[4];
-                drop_words(d, (u32)row, (rows.c0 + c) >> 3, bits);
-                drop_apply(d, bits, g[k]);
+            for (int k0 = 0; k0 < NV; k0 += N) {
+                u32 rws[N], groups[N], bits[N][4];
+#pragma unroll
+                for (int k = 0; k < N; k++) rws[k] = (u32)row, groups[k] = (rows.c0 + block_column<NV>(k0 + k, rg.t)) >> 3;
+                drop_words<N>(d, rws, groups, bits);
+#pragma unroll
+                for (int k = 0; k < N; k++)
+#pragma unroll
+                    for (int e = 0; e < 8; e++) g[k0 + k][e] = dropped(d, bits[k], e) ? 0.f : g[k0 + k][e];
             }
-            exp_about(p[k], lse);
-            mask_from(p[k], c, end, 0.f);
-#pragma unroll
-            for (int e = 0; e < 8; e++) dot = fmaf(p[k][e], g[k][e], dot);
         }
+        exp_about<NV>(p, lse == -INFINITY ? 0.f : lse);
+        float dot = 0.f, dot2 = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; k++)
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                dot = fmaf(p[k][e], g[k][e], dot);
+                dot2 = fmaf(p[k][e + 1], g[k][e + 1], dot2);
+            }
+        dot += dot2;
         // A sum's logarithm does not show beside a statistic this large (ulp 2^-9 and up): P is then normalised again.
         // (A property of the row, so that all its threads meet in row_sum.)
         if (lse != -INFINITY && fabsf(lse) > 16384.f) {
@@ -121,12 +139,13 @@ __global__ void __launch_bounds__(THREADS) softmax_backward(const SoftmaxArgs a)
 #pragma unroll
                 for (int e = 0; e < 8; e++) p[k][e] *= f;
         }
-        dot = row_sum(dot);
+        const float factor = DROP ? d.factor : 1.f;
+        dot = row_sum(dot) * factor;
         float carry = 0.f;              // lane 0: the last sum of the block before
 #pragma unroll
         for (int k = 0; k < NV; k++) {
 #pragma unroll
-            for (int e = 0; e < 8; e++) p[k][e] *= g[k][e] - dot;
+            for (int e = 0; e < 8; e++) p[k][e] *= DROP ? fmaf(g[k][e], factor, -dot) : g[k][e] - dot;
             if (a.partial) {
                 const float from = __shfl_sync(kAllLanes, acc[k][7], (rg.lane + 31u) & 31u);
 #pragma unroll
@@ -147,11 +166,9 @@ __global__ void __launch_bounds__(THREADS) softmax_backward(const SoftmaxArgs a)
 #pragma unroll
         for (int k = 0; k < NV; k++)
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                put((int)(rows.c0 + block_column<NV>(k, rg.t)) + e - pos, acc[k][e]);
-                __syncwarp();
-            }
+            for (int e = 0; e < 8; e++) put((int)(rows.c0 + block_column<NV>(k, rg.t)) + e - pos, acc[k][e]);
     }
+    after_kernel_may_start();
     before = warp_sum(before);
     behind = warp_sum(behind);
     if (rg.lane == 0) ends[cta_warp] = make_float2(before, behind);
@@ -185,24 +202,28 @@ __global__ void __launch_bounds__(THREADS) softmax_backward(const SoftmaxArgs a)
     }
 }
 
-constexpr int kTableSumWarps = 8;
+constexpr int kTableSumWarps = 32;
 
-// dtable[b][head]: the groups' sums of that head over the batch, in their order.
+// dtable[b][head]: the sums of that head's CTAs (`per` of each sequence's), in their order.
 __global__ void __launch_bounds__(32 * kTableSumWarps)
 softmax_back_sum(const float *partial, float *dtable, u32 batch, u32 heads, u32 per, u32 buckets)
 {
     __shared__ float sums[kTableSumWarps][33];
     const u32 head = blockIdx.x, lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, b = blockIdx.y * 32u + lane;
+    wait_for_kernel_before();
     float s = 0.f;
-    if (b < buckets)
+    if (b < buckets) {
+#pragma unroll 8
         for (u64 j = warp; j < (u64)batch * per; j += kTableSumWarps) {
-            const u64 bh = (j / per) * heads + head;
-            s += partial[(bh * per + j % per) * buckets + b];
+            const u64 n = j / per;
+            s += partial[((n * heads + head) * per + (j - n * per)) * buckets + b];
         }
+    }
     sums[warp][lane] = s;
     __syncthreads();
     if (warp != 0 || b >= buckets) return;
     s = 0.f;
+#pragma unroll
     for (int w = 0; w < kTableSumWarps; w++) s += sums[w][lane];
     dtable[(u64)b * heads + head] = s;
 }
@@ -243,8 +264,8 @@ int launch_softmax_back(SoftmaxArgs &a, u32 type, cudaStream_t st)
         else launch_type<ADACOMP_TYPE_F16>(a, st);
     }
     if (a.table && a.dtable && a.heads)
-        softmax_back_sum<<<dim3(a.heads, (a.buckets + 31u) / 32u), 32 * kTableSumWarps, 0, st>>>(
-            a.partial, a.dtable, any ? a.batch : 0u, a.heads, a.chunks * a.cluster, a.buckets);
+        launch_after(softmax_back_sum, dim3(a.heads, (a.buckets + 31u) / 32u), 32 * kTableSumWarps, st, (const float *)a.partial,
+                     a.dtable, any ? a.batch : 0u, a.heads, a.chunks * a.cluster, a.buckets);
     return launched();
 }
 
