@@ -137,8 +137,8 @@ size_t adacomp_layer_norm_workspace(uint64_t rows, uint32_t cols)
     NormArgs a = {};
     a.rows = rows;
     a.cols = cols;
-    norm_split(a);
-    return (size_t)(a.partials ? a.partials : 1u) * 2 * cols * sizeof(float);
+    norm_split(a, true);
+    return (size_t)(a.sets ? a.sets : 1u) * 2 * cols * sizeof(float);
 }
 
 int adacomp_layer_norm_backward(const void *dy, const void *dh_in, const void *h, const void *weight, const float *mean,

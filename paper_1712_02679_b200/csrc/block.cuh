@@ -98,6 +98,74 @@ template <u32 TYPE> __device__ inline void store1(void *base, u64 e, float v)
 }
 
 // ---------------------------------------------------------------------------------
+// two binary32 operations in one instruction (PTX .f32x2, sm_100): these kernels are bound by how many instructions an SM
+// issues, not by how many operations it has units for
+// ---------------------------------------------------------------------------------
+
+__device__ inline void fma2(float &d0, float &d1, float a0, float a1, float b0, float b1, float c0, float c1)
+{
+    asm("{\n\t.reg .b64 a, b, c, d;\n\t"
+        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d0), "=f"(d1)
+        : "f"(a0), "f"(a1), "f"(b0), "f"(b1), "f"(c0), "f"(c1));
+}
+
+__device__ inline void mul2(float &d0, float &d1, float a0, float a1, float b0, float b1)
+{
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "mul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d0), "=f"(d1)
+        : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+
+__device__ inline void add2(float &d0, float &d1, float a0, float a1, float b0, float b1)
+{
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d0), "=f"(d1)
+        : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+
+// v = v * x + y, v * x, v + x, element by element or with one number
+__device__ inline void fma8(float (&v)[8], float x, float y)
+{
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) fma2(v[e], v[e + 1], v[e], v[e + 1], x, x, y, y);
+}
+__device__ inline void mul8(float (&v)[8], float x)
+{
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) mul2(v[e], v[e + 1], v[e], v[e + 1], x, x);
+}
+__device__ inline void mul8(float (&v)[8], const float (&x)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) mul2(v[e], v[e + 1], v[e], v[e + 1], x[e], x[e + 1]);
+}
+__device__ inline void add8(float (&v)[8], float x)
+{
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) add2(v[e], v[e + 1], v[e], v[e + 1], x, x);
+}
+__device__ inline void add8(float (&v)[8], const float (&x)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) add2(v[e], v[e + 1], v[e], v[e + 1], x[e], x[e + 1]);
+}
+// acc += v, acc += v * x
+__device__ inline void sum8(float2 &acc, const float (&v)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) add2(acc.x, acc.y, acc.x, acc.y, v[e], v[e + 1]);
+}
+__device__ inline void dot8(float2 &acc, const float (&v)[8], const float (&x)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) fma2(acc.x, acc.y, v[e], v[e + 1], x[e], x[e + 1], acc.x, acc.y);
+}
+
+// ---------------------------------------------------------------------------------
 // how a row's threads share its columns
 //
 // A row belongs to `tpr` threads (whole warps); each holds NV blocks of eight neighbouring columns.  A warp's blocks lie
@@ -340,7 +408,12 @@ __device__ inline bool dropped(const Drop &d, const u32 (&w)[4], int e)
 __device__ inline void drop_apply(const Drop &d, const u32 (&w)[4], float (&v)[8])
 {
 #pragma unroll
-    for (int e = 0; e < 8; e++) v[e] = dropped(d, w, e) ? 0.f : v[e] * d.factor;
+    for (int e = 0; e < 8; e += 2) {
+        float x, y;
+        mul2(x, y, v[e], v[e + 1], d.factor, d.factor);
+        v[e] = dropped(d, w, e) ? 0.f : x;
+        v[e + 1] = dropped(d, w, e + 1) ? 0.f : y;
+    }
 }
 
 // ---------------------------------------------------------------------------------
@@ -362,15 +435,25 @@ __device__ inline float warp_max(float v)
     return m;
 }
 
-// Two sums over the warp for little more than the price of one: the first step leaves a's terms in the lower half of the
-// lanes and b's in the upper half.  Returns sum(a) to lanes 0..15, sum(b) to lanes 16..31.
-__device__ inline float warp_two_sums(float a, float b, u32 lane)
+// N sums over the warp at once (N = 1, 2, 4 or 8).  While there are several values left, a step halves them: a lane keeps
+// one half of the values and gives away the other, so that N sums take N + 4 - log2 N exchanges instead of 5 N.  Returns
+// the sum of value lane / (32 / N).
+template <int N> __device__ inline float warp_sums(const float (&v)[N], u32 lane)
 {
-    const bool up = lane & 16u;
-    float v = (up ? b : a) + __shfl_xor_sync(kAllLanes, up ? a : b, 16);
+    float x[N];
 #pragma unroll
-    for (int d = 8; d > 0; d >>= 1) v += __shfl_xor_sync(kAllLanes, v, d);
-    return v;
+    for (int i = 0; i < N; i++) x[i] = v[i];
+    int d = 16;
+#pragma unroll
+    for (int n = N; n > 1; n /= 2, d /= 2) {
+        const bool up = lane & d;
+#pragma unroll
+        for (int i = 0; i < n / 2; i++)
+            x[i] = (up ? x[i + n / 2] : x[i]) + __shfl_xor_sync(kAllLanes, up ? x[i] : x[i + n / 2], d);
+    }
+#pragma unroll
+    for (; d > 0; d /= 2) x[0] += __shfl_xor_sync(kAllLanes, x[0], d);
+    return x[0];
 }
 
 // The sum over each half of the warp.
@@ -398,6 +481,35 @@ struct RowGroup {
         else asm volatile("bar.sync %0, %1;" ::"r"(g + 1u), "r"(tpr) : "memory");
     }
 };
+
+// Where the warps of a row leave N values for one another: slots of 16, those of missing warps zero.
+template <int N> struct RowSlots { float v[N][16]; };
+
+// The sums of N values over the threads of a row, in all of them.  `slots`: this row's; the caller alternates between two
+// sets and clears both before the first use.
+template <int N> __device__ inline void row_sums(float (&v)[N], const RowGroup &rg, RowSlots<N> &slots)
+{
+    constexpr u32 span = 32 / N;                // lanes that share a value
+    const u32 which = rg.lane / span, j = rg.lane % span;
+    float x = warp_sums<N>(v, rg.lane);
+    if (rg.warps > 1) {
+        if (j == 0) slots.v[which][rg.warp] = x;
+        rg.sync();
+        if constexpr (span >= 16) {
+            x = j < 16 ? slots.v[which][j] : 0.f;
+        } else if constexpr (span == 8) {
+            const float2 p = reinterpret_cast<const float2 *>(slots.v[which])[j];
+            x = p.x + p.y;
+        } else {
+            const float4 p = reinterpret_cast<const float4 *>(slots.v[which])[j];
+            x = (p.x + p.y) + (p.z + p.w);
+        }
+#pragma unroll
+        for (int d = (span > 16 ? 16 : (int)span) / 2; d > 0; d /= 2) x += __shfl_xor_sync(kAllLanes, x, d);
+    }
+#pragma unroll
+    for (int i = 0; i < N; i++) v[i] = from_lane(x, i * (int)span);
+}
 
 // n / d for n < 2^31 by a multiplication (Granlund and Montgomery, "Division by invariant integers using
 // multiplication", 1994)

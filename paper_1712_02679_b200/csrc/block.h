@@ -39,11 +39,12 @@ struct NormArgs {
     float *mean, *rstd;
     const void *dy, *dh_in;                      // backward
     void *dx, *dresidual, *dweight, *dbias;
-    float *partial;                              // [partials][2][cols]: sums of each CTA's rows
+    float *partial;                              // [sets][2][cols]: sums of each CTA's rows
     u64 rows;
     u32 cols, param_type;
-    // norm_split: threads per row, blocks of eight per thread, rows per CTA, CTAs per row, columns per CTA
-    u32 tpr, per, groups, cluster, slice, partials;
+    // norm_split: threads per row, blocks of eight per thread, most threads of a CTA, rows that a CTA works on side by side,
+    // CTAs per row, columns per CTA, and how many such sets of rows are worked on at once
+    u32 tpr, per, threads, groups, cluster, slice, sets;
     float eps;
     DropArgs drop;
 };
@@ -51,7 +52,7 @@ struct NormArgs {
 // norm.cu, norm_back.cu
 int launch_norm(NormArgs &a, u32 type, cudaStream_t st);
 int launch_norm_back(NormArgs &a, u32 type, cudaStream_t st);
-void norm_split(NormArgs &a);
+void norm_split(NormArgs &a, bool back);
 
 struct SoftmaxArgs {
     const void *scores;

@@ -8,13 +8,16 @@ namespace adacomp_impl {
 namespace cg = cooperative_groups;
 
 constexpr int kNormThreads = 512;            // most threads of a CTA
+constexpr int kNormMany = 256;               // threads of a CTA where there are many rows
+constexpr u32 kNormBusy = 8;                 // warps per SM that make many rows of them
 
-// Launches `kernel` over `rows_at_once` sets of rows, `cluster` CTAs to a row.
-template <typename K> inline void launch_norm_kernel(K kernel, const NormArgs &a, u32 sets, cudaStream_t st)
+template <typename K> inline void launch_norm_kernel(K kernel, const NormArgs &a, size_t smem, cudaStream_t st)
 {
+    if (smem > 16 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(sets * a.cluster);
+    cfg.gridDim = dim3(a.sets * a.cluster);
     cfg.blockDim = dim3(a.tpr * a.groups);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;

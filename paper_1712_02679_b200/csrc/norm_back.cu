@@ -3,130 +3,137 @@
 #include "norm.cuh"
 
 #ifndef NBB
-#define NBB 1
+#define NBB 2
+#endif
+#ifndef PREB
+#define PREB 1
 #endif
 namespace adacomp_impl {
 
 // With xhat = (h - mean) rstd and g = dy weight:  dh = rstd (g - mean(g) - xhat mean(g xhat)) + dh_in.
 // A thread keeps its columns from row to row, so that dweight = sum dy xhat and dbias = sum dy grow in its registers; a
 // CTA leaves one line of each, and norm_back_sum adds the lines in their order.
-template <u32 TYPE, bool ALIGNED, int NV, bool DROP>
-__global__ void __launch_bounds__(kNormThreads, NBB) norm_backward(const NormArgs a)
+template <u32 TYPE, bool ALIGNED, int NV, bool DROP, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? NBB : 1) norm_backward(const NormArgs a)
 {
-    __shared__ float part[2][kNormThreads / 32][2];
+    extern __shared__ float4 params[];
+    __shared__ RowSlots<2> slots[2][THREADS / 64];
     __shared__ float2 peers[2][8];
-    __shared__ float merge[NV == 1 ? kNormThreads * 8 : 1];
+    __shared__ float merge[THREADS * 8];
     const RowGroup rg(a.tpr);
     const u32 rank = a.cluster > 1 ? cg::this_cluster().block_rank() : 0u;
-    if (a.cluster > 1) cg::this_cluster().sync();      // every CTA of the cluster runs before its memory is written
     const u32 c0 = rank * a.slice, cols = min(a.slice, a.cols - c0);
+    const u32 c = block_column<NV>(0, rg.t);                // block k starts at c + 256 k
     const u32 set = blockIdx.x / a.cluster;
-    const u64 step = (u64)a.partials * a.groups;
-    u64 row = (u64)set * a.groups + rg.g;
+    const u64 step = (u64)a.sets * a.groups, step_at = step * a.cols;
+    u64 row = (u64)set * a.groups + rg.g, at = row * a.cols + c0;
     Raw<TYPE, ALIGNED> ry[NV], rh[NV], ri[NV];
     clear(ry);
     clear(rh);
     clear(ri);
     float next_mean = 0.f, next_rstd = 0.f;
-    auto fetch_row = [&](u64 r) {
+    auto fetch_row = [&](u64 r, u64 r_at) {
         const u32 end = r < a.rows ? cols : 0u;
         if (r < a.rows) next_mean = a.mean[r], next_rstd = a.rstd[r];
 #pragma unroll
         for (int k = 0; k < NV; k++) {
-            const u32 c = block_column<NV>(k, rg.t);
-            fetch<TYPE, ALIGNED>(ry[k], a.dy, r * a.cols + c0, c, end);
-            fetch<TYPE, ALIGNED>(rh[k], a.x, r * a.cols + c0, c, end);
-            if (a.dh_in) fetch<TYPE, ALIGNED>(ri[k], a.dh_in, r * a.cols + c0, c, end);
+            fetch<TYPE, ALIGNED>(ry[k], a.dy, r_at, c + 256 * k, end);
+            fetch<TYPE, ALIGNED>(rh[k], a.x, r_at, c + 256 * k, end);
+            if (a.dh_in) fetch<TYPE, ALIGNED>(ri[k], a.dh_in, r_at, c + 256 * k, end);
         }
     };
-    fetch_row(row);
+    constexpr bool PREFETCH = PREB;
+    if (PREFETCH) fetch_row(row, at);
     const void *wp = a.weight ? static_cast<const unsigned char *>(a.weight) + (u64)c0 * type_size(a.param_type) : nullptr;
-    float w[NV][8], dw[NV][8], db[NV][8];
+    float w1[8], dw[NV][8], db[NV][8];
+    const u32 plane = a.tpr * NV;               // blocks of the row's threads
+    if constexpr (NV == 1) {
+        load_param(wp, a.param_type, c, cols, 1.f, w1);
+    } else {
+        for (u32 i = threadIdx.x; i < plane; i += blockDim.x) {
+            load_param(wp, a.param_type, 8 * i, cols, 1.f, w1);
+            params[i] = make_float4(w1[0], w1[1], w1[2], w1[3]);
+            params[plane + i] = make_float4(w1[4], w1[5], w1[6], w1[7]);
+        }
+    }
 #pragma unroll
-    for (int k = 0; k < NV; k++) {
-        load_param(wp, a.param_type, block_column<NV>(k, rg.t), cols, 1.f, w[k]);
+    for (int k = 0; k < NV; k++)
 #pragma unroll
         for (int e = 0; e < 8; e++) dw[k][e] = db[k][e] = 0.f;
-    }
+    for (u32 i = threadIdx.x; i < sizeof(slots) / 4; i += blockDim.x) reinterpret_cast<float *>(slots)[i] = 0.f;
+    __syncthreads();
+    if (a.cluster > 1) cg::this_cluster().sync();      // every CTA of the cluster runs before its memory is written
     Drop d;
     if constexpr (DROP) d = drop_begin(a.drop);
     const float inv_cols = 1.f / (float)a.cols;
     u32 parity = 0;
 #pragma unroll 1
-    for (; row < a.rows; row += step, parity ^= 1u) {
-        const u64 at = row * a.cols + c0;
-        float g[NV][8], xh[NV][8];
+    for (; row < a.rows; row += step, at += step_at, parity ^= 1u) {
+        if (!PREFETCH) fetch_row(row, at);
+        float g[NV][8], xh[NV][8], in[NV][8];
         const float mean = next_mean, rstd = next_rstd;
-        float s1 = 0.f, s2 = 0.f;
+        float2 s1 = make_float2(0.f, 0.f), s2 = make_float2(0.f, 0.f);
 #pragma unroll
         for (int k = 0; k < NV; k++) {
             unpack<TYPE, ALIGNED>(ry[k], at, g[k]);
             unpack<TYPE, ALIGNED>(rh[k], at, xh[k]);
+            if (a.dh_in) unpack<TYPE, ALIGNED>(ri[k], at, in[k]);
             if constexpr (!ALIGNED) {           // (blocks of an ALIGNED row are whole or hold zeros)
-                mask_from(g[k], block_column<NV>(k, rg.t), cols, 0.f);
-                mask_from(xh[k], block_column<NV>(k, rg.t), cols, 0.f);
-            }
-#pragma unroll
-            for (int e = 0; e < 8; e++) {       // (beyond the row's end g is 0, so that xhat does not matter)
-                xh[k][e] = (xh[k][e] - mean) * rstd;
-                dw[k][e] = fmaf(g[k][e], xh[k][e], dw[k][e]);
-                db[k][e] += g[k][e];
-                g[k][e] *= w[k][e];
-                s1 += g[k][e];
-                s2 = fmaf(g[k][e], xh[k][e], s2);
+                mask_from(g[k], c + 256 * k, cols, 0.f);
+                mask_from(xh[k], c + 256 * k, cols, 0.f);
             }
         }
-        float in[NV][8];
-        if (a.dh_in) {
-#pragma unroll
-            for (int k = 0; k < NV; k++) unpack<TYPE, ALIGNED>(ri[k], at, in[k]);
-        }
-        fetch_row(row + step);          // the next row is on its way while this one is worked on
-        float v = warp_two_sums(s1, s2, rg.lane);
-        if (rg.warps > 1) {
-            if ((rg.lane & 15u) == 0) part[parity][rg.first_warp + rg.warp][rg.lane >> 4] = v;
-            rg.sync();
-            const u32 i = rg.lane & 15u;
-            v = half_sum(i < rg.warps ? part[parity][rg.first_warp + i][rg.lane >> 4] : 0.f);
-        }
-        s1 = from_lane(v, 0);
-        s2 = from_lane(v, 16);
-        if (a.cluster > 1) {
-            cg::cluster_group cl = cg::this_cluster();
-            if (threadIdx.x < a.cluster) cl.map_shared_rank(&peers[parity][0], threadIdx.x)[rank] = make_float2(s1, s2);
-            cl.sync();
-            s1 = s2 = 0.f;
-            for (u32 i = 0; i < a.cluster; i++) {
-                s1 += peers[parity][i].x;
-                s2 += peers[parity][i].y;
-            }
-        }
-        s1 *= inv_cols;
-        s2 *= inv_cols;
+        if (PREFETCH) fetch_row(row + step, at + step_at);      // the next row is on its way while this one is worked on
 #pragma unroll
         for (int k = 0; k < NV; k++) {
+            add8(xh[k], -mean);                 // (beyond the row's end g is 0, so that xhat does not matter)
+            mul8(xh[k], rstd);
 #pragma unroll
-            for (int e = 0; e < 8; e++) g[k][e] = fmaf(-xh[k][e], s2, g[k][e] - s1);
+            for (int e = 0; e < 8; e += 2)
+                fma2(dw[k][e], dw[k][e + 1], g[k][e], g[k][e + 1], xh[k][e], xh[k][e + 1], dw[k][e], dw[k][e + 1]);
+            add8(db[k], g[k]);
+            if constexpr (NV == 1) {
+                mul8(g[k], w1);
+            } else {
+                const u32 i = c / 8 + 32 * k;
+                const float4 x = params[i], y = params[plane + i];
+                const float w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                mul8(g[k], w);
+            }
+            sum8(s1, g[k]);
+            dot8(s2, g[k], xh[k]);
+        }
+        float s[2] = {s1.x + s1.y, s2.x + s2.y};
+        row_sums<2>(s, rg, slots[parity][rg.warps > 1 ? rg.g : 0u]);
+        if (a.cluster > 1) {
+            cg::cluster_group cl = cg::this_cluster();
+            if (threadIdx.x < a.cluster) cl.map_shared_rank(&peers[parity][0], threadIdx.x)[rank] = make_float2(s[0], s[1]);
+            cl.sync();
+            s[0] = s[1] = 0.f;
+            for (u32 j = 0; j < a.cluster; j++) {
+                s[0] += peers[parity][j].x;
+                s[1] += peers[parity][j].y;
+            }
+        }
+        const float m1 = -s[0] * inv_cols, m2 = -s[1] * inv_cols;
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+            add8(g[k], m1);
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) fma2(g[k][e], g[k][e + 1], xh[k][e], xh[k][e + 1], m2, m2, g[k][e], g[k][e + 1]);
             if (a.dh_in) {
 #pragma unroll
-                for (int e = 0; e < 8; e++) g[k][e] = fmaf(g[k][e], rstd, in[k][e]);
+                for (int e = 0; e < 8; e += 2) fma2(g[k][e], g[k][e + 1], g[k][e], g[k][e + 1], rstd, rstd, in[k][e], in[k][e + 1]);
             } else {
-#pragma unroll
-                for (int e = 0; e < 8; e++) g[k][e] *= rstd;
+                mul8(g[k], rstd);
             }
-            if (a.dresidual) store_block<TYPE, ALIGNED>(a.dresidual, at, block_column<NV>(k, rg.t), cols, g[k]);
-        }
-        if constexpr (DROP) {
-            u32 rows[NV], groups[NV], bits[NV][4];
-#pragma unroll
-            for (int k = 0; k < NV; k++) rows[k] = (u32)row, groups[k] = (c0 + block_column<NV>(k, rg.t)) >> 3;
-            drop_words<NV>(d, rows, groups, bits);
-#pragma unroll
-            for (int k = 0; k < NV; k++) drop_apply(d, bits[k], g[k]);
-        }
-        if (a.dx) {
-#pragma unroll
-            for (int k = 0; k < NV; k++) store_block<TYPE, ALIGNED>(a.dx, at, block_column<NV>(k, rg.t), cols, g[k]);
+            if (a.dresidual) store_block<TYPE, ALIGNED>(a.dresidual, at, c + 256 * k, cols, g[k]);
+            if constexpr (DROP) {
+                u32 bits[4];
+                drop_words(d, (u32)row, (c0 + c + 256 * k) >> 3, bits);
+                drop_apply(d, bits, g[k]);
+            }
+            if (a.dx) store_block<TYPE, ALIGNED>(a.dx, at, c + 256 * k, cols, g[k]);
         }
     }
     after_kernel_may_start();
@@ -136,21 +143,24 @@ __global__ void __launch_bounds__(kNormThreads, NBB) norm_backward(const NormArg
 #pragma unroll
     for (int which = 0; which < 2; which++) {
         float(&acc)[NV][8] = which ? db : dw;
-        if (NV == 1 && a.groups > 1) {          // rows of the CTA's groups, added in their order
-            __syncthreads();
+        if (a.groups > 1) {          // rows of the CTA's groups, added in their order
 #pragma unroll
-            for (int e = 0; e < 8; e++) merge[e * kNormThreads + threadIdx.x] = acc[0][e];
-            __syncthreads();
-            if (rg.g == 0) {
-                for (u32 g = 1; g < a.groups; g++)
+            for (int k = 0; k < NV; k++) {
+                __syncthreads();
 #pragma unroll
-                    for (int e = 0; e < 8; e++) acc[0][e] += merge[e * kNormThreads + g * rg.tpr + rg.t];
+                for (int e = 0; e < 8; e++) merge[e * THREADS + threadIdx.x] = acc[k][e];
+                __syncthreads();
+                if (rg.g == 0) {
+                    for (u32 g = 1; g < a.groups; g++)
+#pragma unroll
+                        for (int e = 0; e < 8; e++) acc[k][e] += merge[e * THREADS + g * rg.tpr + rg.t];
+                }
             }
         }
         if (rg.g == 0) {
 #pragma unroll
             for (int k = 0; k < NV; k++)
-                store_block<ADACOMP_TYPE_F32, ALIGNED>(out, line + (u64)which * a.cols, block_column<NV>(k, rg.t), cols, acc[k]);
+                store_block<ADACOMP_TYPE_F32, ALIGNED>(out, line + (u64)which * a.cols, c + 256 * k, cols, acc[k]);
         }
     }
 }
@@ -183,22 +193,29 @@ __global__ void __launch_bounds__(32 * kSumWarps) norm_back_sum(const float *par
     else store1<ADACOMP_TYPE_F16>(out, c, s);
 }
 
-template <u32 TYPE, bool ALIGNED, int NV> static void launch_drop(const NormArgs &a, cudaStream_t st)
+template <u32 TYPE, bool ALIGNED, int NV, int THREADS> static void launch_drop(const NormArgs &a, cudaStream_t st)
 {
-    if (a.drop.threshold) launch_norm_kernel(norm_backward<TYPE, ALIGNED, NV, true>, a, a.partials, st);
-    else launch_norm_kernel(norm_backward<TYPE, ALIGNED, NV, false>, a, a.partials, st);
+    const size_t smem = NV == 1 ? 0 : (size_t)a.tpr * NV * 32;
+    if (a.drop.threshold) launch_norm_kernel(norm_backward<TYPE, ALIGNED, NV, true, THREADS>, a, smem, st);
+    else launch_norm_kernel(norm_backward<TYPE, ALIGNED, NV, false, THREADS>, a, smem, st);
+}
+
+template <u32 TYPE, bool ALIGNED> static void launch_blocks(const NormArgs &a, cudaStream_t st)
+{
+    const bool small = a.threads == kNormMany;
+    if (a.per == 2u) small ? launch_drop<TYPE, ALIGNED, 2, kNormMany>(a, st) : launch_drop<TYPE, ALIGNED, 2, kNormThreads>(a, st);
+    else small ? launch_drop<TYPE, ALIGNED, 1, kNormMany>(a, st) : launch_drop<TYPE, ALIGNED, 1, kNormThreads>(a, st);
 }
 
 template <u32 TYPE> static void launch_type(const NormArgs &a, cudaStream_t st)
 {
-    const bool two = a.per == 2u;
-    if (a.cols % 8u == 0) two ? launch_drop<TYPE, true, 2>(a, st) : launch_drop<TYPE, true, 1>(a, st);
-    else two ? launch_drop<TYPE, false, 2>(a, st) : launch_drop<TYPE, false, 1>(a, st);
+    if (a.cols % 8u == 0) launch_blocks<TYPE, true>(a, st);
+    else launch_blocks<TYPE, false>(a, st);
 }
 
 int launch_norm_back(NormArgs &a, u32 type, cudaStream_t st)
 {
-    norm_split(a);
+    norm_split(a, true);
     if (!a.dweight && !a.dbias) a.partial = nullptr;
     if (a.rows) {
         if (type == ADACOMP_TYPE_F32) launch_type<ADACOMP_TYPE_F32>(a, st);
@@ -207,7 +224,7 @@ int launch_norm_back(NormArgs &a, u32 type, cudaStream_t st)
     }
     if (a.partial)
         launch_after(norm_back_sum, dim3((a.cols + 31u) / 32u, 2), 32 * kSumWarps, st, (const float *)a.partial,
-                     a.rows ? a.partials : 0u, a.cols, a.dweight, a.dbias, a.param_type);
+                     a.rows ? a.sets : 0u, a.cols, a.dweight, a.dbias, a.param_type);
     return launched();
 }
 
