@@ -137,7 +137,7 @@ size_t adacomp_layer_norm_workspace(uint64_t rows, uint32_t cols)
     NormArgs a = {};
     a.rows = rows;
     a.cols = cols;
-    norm_split(a, true);
+    norm_split(a, kNormBackBlocks);
     return (size_t)(a.sets ? a.sets : 1u) * 2 * cols * sizeof(float);
 }
 
@@ -209,14 +209,15 @@ int adacomp_bias_softmax(const void *scores, const float *table, const adacomp_r
 size_t adacomp_bias_softmax_workspace(uint32_t batch, uint32_t heads, uint32_t q_len, uint32_t k_len,
                                       const adacomp_relpos *relpos)
 {
-    if (!relpos || k_len > ADACOMP_MAX_KEYS || relpos->num_buckets > ADACOMP_MAX_BUCKETS) return 0;
+    adacomp_softmax_options opt = {};
+    opt.batch = batch;
+    opt.heads = heads;
+    opt.q_len = q_len;
+    opt.k_len = k_len;
+    opt.ld = k_len;
     SoftmaxArgs a = {};
-    a.batch = batch;
-    a.heads = heads;
-    a.q_len = q_len;
-    a.k_len = k_len;
-    softmax_split(a);
-    const size_t bytes = (size_t)batch * heads * a.chunks * a.cluster * relpos->num_buckets * sizeof(float);
+    if (!relpos || check_softmax(reinterpret_cast<const float *>(16), relpos, &opt, a) != ADACOMP_OK) return 0;
+    const size_t bytes = softmax_workspace(a);
     return bytes ? bytes : 16;
 }
 

@@ -102,6 +102,11 @@ template <u32 TYPE> __device__ inline void store1(void *base, u64 e, float v)
 // issues, not by how many operations it has units for
 // ---------------------------------------------------------------------------------
 
+#ifdef SCALAR
+__device__ inline void fma2(float &d0, float &d1, float a0, float a1, float b0, float b1, float c0, float c1) { d0 = fmaf(a0,b0,c0); d1 = fmaf(a1,b1,c1); }
+__device__ inline void mul2(float &d0, float &d1, float a0, float a1, float b0, float b1) { d0 = a0*b0; d1 = a1*b1; }
+__device__ inline void add2(float &d0, float &d1, float a0, float a1, float b0, float b1) { d0 = a0+b0; d1=a1+b1; }
+#else
 __device__ inline void fma2(float &d0, float &d1, float a0, float a1, float b0, float b1, float c0, float c1)
 {
     asm("{\n\t.reg .b64 a, b, c, d;\n\t"
@@ -127,6 +132,7 @@ __device__ inline void add2(float &d0, float &d1, float a0, float a1, float b0, 
         : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
 }
 
+#endif
 // v = v * x + y, v * x, v + x, element by element or with one number
 __device__ inline void fma8(float (&v)[8], float x, float y)
 {
@@ -187,29 +193,75 @@ template <u32 TYPE> __host__ __device__ constexpr u32 chunk_elems() { return 16u
 // A block as loaded, not yet shifted (what a prefetch holds).
 template <u32 TYPE, bool ALIGNED> struct Raw { uint4 q[(TYPE == ADACOMP_TYPE_F32 ? 2 : 1) + (ALIGNED ? 0 : 1)]; };
 
-template <u32 TYPE, bool ALIGNED, int NV> __device__ inline void clear(Raw<TYPE, ALIGNED> (&r)[NV])
-{
-#pragma unroll
-    for (int k = 0; k < NV; k++)
-#pragma unroll
-        for (int i = 0; i < (int)(sizeof(r[k].q) / 16); i++) r[k].q[i] = make_uint4(0u, 0u, 0u, 0u);
-}
-
-// The block from column c of the row at element row_at, as far as it lies before column `end`; chunks that are not loaded
-// keep what they held.
-template <u32 TYPE, bool ALIGNED>
-__device__ inline void fetch(Raw<TYPE, ALIGNED> &r, const void *base, u64 row_at, u32 c, u32 end)
+// The chunks of the block from column c of the row at element row_at, as far as they lie before column `end`:
+// f(i, address) for each that holds one of its elements.
+template <u32 TYPE, bool ALIGNED, typename F>
+__device__ inline void for_chunks(const void *base, u64 row_at, u32 c, u32 end, F f)
 {
     constexpr u32 per = chunk_elems<TYPE>();
     const u32 s = ALIGNED ? 0u : (u32)row_at & (per - 1u);
     const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const unsigned char *>(base) + (row_at + c - s) * type_size(TYPE));
-    constexpr int n = sizeof(r.q) / 16;
+    constexpr int n = sizeof(Raw<TYPE, ALIGNED>) / 16;
 #pragma unroll
-    for (int i = 0; i < n; i++) {
-        // chunk i holds columns c - s + i * per and up (the first one: column c)
-        if (c + (i ? i * per - s : 0u) < end && (ALIGNED || i * per - s < 8u || i == 0)) r.q[i] = p[i];
-    }
+    for (int i = 0; i < n; i++)     // chunk i holds columns c - s + i * per and up (the first one: column c)
+        if (c + (i ? i * per - s : 0u) < end && (ALIGNED || i * per - s < 8u || i == 0)) f(i, p + i);
 }
+
+// Into registers; what is not loaded keeps what it held.
+template <u32 TYPE, bool ALIGNED>
+__device__ inline void fetch(Raw<TYPE, ALIGNED> &r, const void *base, u64 row_at, u32 c, u32 end)
+{
+    for_chunks<TYPE, ALIGNED>(base, row_at, c, end, [&](int i, const uint4 *p) { r.q[i] = *p; });
+}
+
+// Rows on their way: each thread copies its own chunks of the next rows into its own places of shared memory
+// (cp.async) and reads them back itself, so that nobody waits for anybody, and no register holds what has not arrived.
+// `arrays` tensors, STAGES rows of each: with two, the next row is copied while one is worked on; with one, for the widest
+// rows, only once its places have been read.
+template <u32 TYPE, bool ALIGNED, int NV, int THREADS, int STAGES> struct Ring {
+    static constexpr int kChunks = sizeof(Raw<TYPE, ALIGNED>) / 16;
+    static constexpr u32 kArray = NV * kChunks * THREADS;          // in 16 bytes
+    static constexpr size_t bytes(u32 arrays) { return (size_t)STAGES * arrays * kArray * 16; }
+    uint4 *mine;
+    u32 arrays;
+    __device__ uint4 *place(u32 turn, u32 array) const { return mine + ((turn & (STAGES - 1)) * arrays + array) * kArray; }
+    __device__ uint4 *end() const { return mine - threadIdx.x + STAGES * arrays * kArray; }
+    // What was asked for before the last request has arrived (one stage: the last request itself).
+    __device__ static void wait()
+    {
+        if (STAGES == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 0;" ::: "memory");
+    }
+    // Blocks k = 0, 1, .. start at columns c + 256 k.
+    __device__ static void copy(uint4 *to, const void *base, u64 row_at, u32 c, u32 end)
+    {
+#pragma unroll
+        for (int k = 0; k < NV; k++)
+            for_chunks<TYPE, ALIGNED>(base, row_at, c + 256 * k, end, [&](int i, const uint4 *p) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(to + (k * kChunks + i) * THREADS)), "l"(p)
+                             : "memory");
+            });
+    }
+    __device__ static Raw<TYPE, ALIGNED> take(const uint4 *from, int k)
+    {
+        Raw<TYPE, ALIGNED> r;
+#pragma unroll
+        for (int i = 0; i < kChunks; i++) r.q[i] = from[(k * kChunks + i) * THREADS];
+        return r;
+    }
+    // Places that no copy reaches, where the kernel counts on zeros behind a row's end.
+    __device__ void clear(u32 c, u32 end) const
+    {
+        for (u32 j = 0; j < STAGES * arrays; j++)
+#pragma unroll
+            for (int k = 0; k < NV; k++)
+#pragma unroll
+                for (int i = 0; i < kChunks; i++)
+                    if (c + 256 * k >= end) mine[j * kArray + (k * kChunks + i) * THREADS] = make_uint4(0u, 0u, 0u, 0u);
+    }
+};
+
+__device__ inline void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 
 // w[0..n) = in[shift .. shift + n) for a shift of 0..3 words (the same for the whole warp)
 template <int N, int M> __device__ inline void shift_words(const u32 (&in)[M], u32 shift, u32 (&out)[N])

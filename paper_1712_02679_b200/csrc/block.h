@@ -52,7 +52,8 @@ struct NormArgs {
 // norm.cu, norm_back.cu
 int launch_norm(NormArgs &a, u32 type, cudaStream_t st);
 int launch_norm_back(NormArgs &a, u32 type, cudaStream_t st);
-void norm_split(NormArgs &a, bool back);
+constexpr u32 kNormBackBlocks = 2;           // blocks of eight per thread in layer norm's backward pass, where there are many rows
+void norm_split(NormArgs &a, u32 most);
 
 struct SoftmaxArgs {
     const void *scores;
@@ -67,7 +68,7 @@ struct SoftmaxArgs {
     u32 batch, heads, q_len, k_len, causal;
     int q_offset;
     // softmax_split: as above; rows a group of threads takes one after the other, and a CTA's chunks per head
-    u32 tpr, per, groups, cluster, slice, run, chunks;
+    u32 tpr, per, threads, groups, cluster, slice, run, chunks;
     float scale;
     DropArgs drop;
     u32 buckets, side, both, reach;              // the bias: see include/adacomp.h (adacomp_relpos)
@@ -77,6 +78,7 @@ struct SoftmaxArgs {
 // softmax.cu, softmax_back.cu
 int launch_softmax(SoftmaxArgs &a, u32 type, cudaStream_t st);
 int launch_softmax_back(SoftmaxArgs &a, u32 type, cudaStream_t st);
-void softmax_split(SoftmaxArgs &a);
+void softmax_split(SoftmaxArgs &a, bool back, bool aligned);
+size_t softmax_workspace(SoftmaxArgs &a);
 
 }  // namespace adacomp_impl

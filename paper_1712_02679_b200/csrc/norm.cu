@@ -1,34 +1,21 @@
 // Layer norm, forward: h = residual + dropout(x), y = (h - mean(h)) / sqrt(var(h) + eps) * weight + bias.
 #include "norm.cuh"
 
-#ifndef NFB
-#define NFB 2
-#endif
-#ifndef NBB
-#define NBB 2
-#endif
-#ifndef NVF
-#define NVF 8u
-#endif
-#ifndef NVB
-#define NVB 2u
-#endif
 namespace adacomp_impl {
 
 // How a row's columns are shared.  Few rows: one thread per eight columns, up to 512 of them, for a short way through the
 // row.  Enough rows to give every SM `kNormBusy` warps of the other kind: threads with more columns each, up to `most`
 // blocks of eight, so that what a row costs besides its elements is shared by many of them.  Wider rows take a cluster of
 // CTAs.
-void norm_split(NormArgs &a, bool back)
+void norm_split(NormArgs &a, u32 most)
 {
     const u32 blocks = (a.cols + 7u) / 8u;
-    const u32 most = back ? NVB : NVF, threads = kNormMany;
     u32 per = 1;
     while (per < most && blocks > 32u * per) per *= 2;
     const u32 warps = (blocks + per * 32u - 1) / (per * 32u);
     const bool many = per > 1 && a.rows * warps >= (u64)kBlockSms * kNormBusy;
     a.per = many ? per : 1u;
-    const u32 cta = many ? threads : (u32)kNormThreads;
+    const u32 cta = many ? kNormMany : kNormThreads;
     a.cluster = 1;
     while (a.cluster < 8u && blocks > a.cluster * cta * a.per) a.cluster *= 2;
     if (blocks > a.cluster * cta * a.per) a.per = 2u;        // (only beyond 32768 columns)
@@ -36,7 +23,8 @@ void norm_split(NormArgs &a, bool back)
     a.tpr = (((a.slice + 7u) / 8u + a.per - 1) / a.per + 31u) & ~31u;
     a.threads = a.tpr <= (u32)kNormMany ? kNormMany : kNormThreads;
     a.groups = a.cluster == 1 ? a.threads / a.tpr : 1u;
-    const u64 sets = (a.rows + a.groups - 1) / a.groups, places = (u64)(a.threads == kNormMany ? (back ? NBB : NFB) : 1u) * kBlockSms / a.cluster;
+    const u64 sets = (a.rows + a.groups - 1) / a.groups;
+    const u64 places = (u64)(a.threads == (u32)kNormMany ? 2u : 1u) * kBlockSms / a.cluster;      // CTAs that fit at once
     a.sets = (u32)(sets < places ? sets : places);
 }
 
@@ -44,31 +32,30 @@ void norm_split(NormArgs &a, bool back)
 // Threads with several blocks read the parameters from shared memory (two planes, the first and the second four of each
 // block, so that neighbouring lanes read neighbouring 16 bytes).
 template <u32 TYPE, bool ALIGNED, int NV, bool DROP, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? NFB : 1) norm_forward(const NormArgs a)
+__global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? 2 : 1) norm_forward(const NormArgs a)
 {
-    extern __shared__ float4 params[];
+    extern __shared__ uint4 dynamic[];
     __shared__ RowSlots<1> slots[2][THREADS / 64];
     __shared__ float peers[2][8];
     const RowGroup rg(a.tpr);
     const u32 rank = a.cluster > 1 ? cg::this_cluster().block_rank() : 0u;
     const u32 c0 = rank * a.slice, cols = min(a.slice, a.cols - c0);
     const u32 c = block_column<NV>(0, rg.t);                // block k starts at c + 256 k
-    Raw<TYPE, ALIGNED> rx[NV], rr[NV];
-    clear(rx);
-    clear(rr);
+    const bool res = a.residual != nullptr;
+    constexpr int STAGES = norm_stages(NV, THREADS);
+    const Ring<TYPE, ALIGNED, NV, THREADS, STAGES> ring = {dynamic + threadIdx.x, res ? 2u : 1u};
+    float4 *params = reinterpret_cast<float4 *>(ring.end());
     const u64 step = (u64)a.sets * a.groups, step_at = step * a.cols;
     u64 row = (u64)(blockIdx.x / a.cluster) * a.groups + rg.g, at = row * a.cols + c0;
+    u32 turn = 0;
     auto fetch_row = [&](u64 r, u64 r_at) {
         const u32 end = r < a.rows ? cols : 0u;
-#pragma unroll
-        for (int k = 0; k < NV; k++) fetch<TYPE, ALIGNED>(rx[k], a.x, r_at, c + 256 * k, end);
-        if (a.residual) {
-#pragma unroll
-            for (int k = 0; k < NV; k++) fetch<TYPE, ALIGNED>(rr[k], a.residual, r_at, c + 256 * k, end);
-        }
+        ring.copy(ring.place(turn, 0), a.x, r_at, c, end);
+        if (res) ring.copy(ring.place(turn, 1), a.residual, r_at, c, end);
+        copies_commit();
     };
-    constexpr bool PREFETCH = NV <= 2;          // (more blocks: enough loads are in flight without)
-    if (PREFETCH) fetch_row(row, at);
+    ring.clear(c, cols);
+    fetch_row(row, at);
     const u64 psize = type_size(a.param_type);
     const void *wp = a.weight ? static_cast<const unsigned char *>(a.weight) + c0 * psize : nullptr;
     const void *bp = a.bias ? static_cast<const unsigned char *>(a.bias) + c0 * psize : nullptr;
@@ -109,25 +96,28 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? NFB : 1) norm_
     };
 #pragma unroll 1
     for (; row < a.rows; row += step, at += step_at) {
-        if (!PREFETCH) fetch_row(row, at);
+        turn ^= 1u;
+        if (STAGES == 2) fetch_row(row + step, at + step_at);   // the next row is on its way while this one is worked on
+        ring.wait();
+        const uint4 *px = ring.place(turn ^ 1u, 0), *pr = ring.place(turn ^ 1u, 1);
         float h[NV][8];
 #pragma unroll
         for (int k = 0; k < NV; k++) {
-            unpack<TYPE, ALIGNED>(rx[k], at, h[k]);
+            unpack<TYPE, ALIGNED>(ring.take(px, k), at, h[k]);
             if constexpr (DROP) {
                 u32 bits[4];
                 drop_words(d, (u32)row, (c0 + c + 256 * k) >> 3, bits);
                 drop_apply(d, bits, h[k]);
             }
-            if (a.residual) {
+            if (res) {
                 float r[8];
-                unpack<TYPE, ALIGNED>(rr[k], at, r);
+                unpack<TYPE, ALIGNED>(ring.take(pr, k), at, r);
                 add8(h[k], r);
             }
             // (blocks of an ALIGNED row are whole or hold the zeros they were cleared to)
             if constexpr (!ALIGNED) mask_from(h[k], c + 256 * k, cols, 0.f);
         }
-        if (PREFETCH) fetch_row(row + step, at + step_at);      // the next row is on its way while this one is worked on
+        if (STAGES == 1) fetch_row(row + step, at + step_at);
         if (a.h) {
 #pragma unroll
             for (int k = 0; k < NV; k++) store_block<TYPE, ALIGNED>(a.h, at, c + 256 * k, cols, h[k]);
@@ -174,7 +164,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? NFB : 1) norm_
 
 template <u32 TYPE, bool ALIGNED, int NV, int THREADS> static void launch_drop(const NormArgs &a, cudaStream_t st)
 {
-    const size_t smem = NV == 1 ? 0 : (size_t)a.tpr * NV * 64;
+    const size_t smem = Ring<TYPE, ALIGNED, NV, THREADS, norm_stages(NV, THREADS)>::bytes(a.residual ? 2u : 1u) + (NV == 1 ? 0 : (size_t)a.tpr * NV * 64);
     if (a.drop.threshold) launch_norm_kernel(norm_forward<TYPE, ALIGNED, NV, true, THREADS>, a, smem, st);
     else launch_norm_kernel(norm_forward<TYPE, ALIGNED, NV, false, THREADS>, a, smem, st);
 }
@@ -182,8 +172,7 @@ template <u32 TYPE, bool ALIGNED, int NV, int THREADS> static void launch_drop(c
 template <u32 TYPE, bool ALIGNED> static void launch_blocks(const NormArgs &a, cudaStream_t st)
 {
     const bool small = a.threads == kNormMany;
-    if (a.per == 8u) launch_drop<TYPE, ALIGNED, 8, kNormMany>(a, st);
-    else if (a.per == 4u) launch_drop<TYPE, ALIGNED, 4, kNormMany>(a, st);
+    if (a.per == 4u) launch_drop<TYPE, ALIGNED, 4, kNormMany>(a, st);
     else if (a.per == 2u) small ? launch_drop<TYPE, ALIGNED, 2, kNormMany>(a, st) : launch_drop<TYPE, ALIGNED, 2, kNormThreads>(a, st);
     else small ? launch_drop<TYPE, ALIGNED, 1, kNormMany>(a, st) : launch_drop<TYPE, ALIGNED, 1, kNormThreads>(a, st);
 }
@@ -197,7 +186,8 @@ template <u32 TYPE> static void launch_type(const NormArgs &a, cudaStream_t st)
 int launch_norm(NormArgs &a, u32 type, cudaStream_t st)
 {
     if (a.rows == 0) return ADACOMP_OK;
-    norm_split(a, false);
+    // (four blocks of unaligned binary32 rows, which take three chunks each, would not fit into shared memory)
+    norm_split(a, a.cols % 8u == 0 || type != ADACOMP_TYPE_F32 ? 4u : 2u);
     if (type == ADACOMP_TYPE_F32) launch_type<ADACOMP_TYPE_F32>(a, st);
     else if (type == ADACOMP_TYPE_BF16) launch_type<ADACOMP_TYPE_BF16>(a, st);
     else launch_type<ADACOMP_TYPE_F16>(a, st);

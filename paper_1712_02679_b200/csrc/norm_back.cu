@@ -2,21 +2,15 @@
 // gradients, which are sums over all rows.
 #include "norm.cuh"
 
-#ifndef NBB
-#define NBB 2
-#endif
-#ifndef PREB
-#define PREB 1
-#endif
 namespace adacomp_impl {
 
 // With xhat = (h - mean) rstd and g = dy weight:  dh = rstd (g - mean(g) - xhat mean(g xhat)) + dh_in.
 // A thread keeps its columns from row to row, so that dweight = sum dy xhat and dbias = sum dy grow in its registers; a
 // CTA leaves one line of each, and norm_back_sum adds the lines in their order.
 template <u32 TYPE, bool ALIGNED, int NV, bool DROP, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? NBB : 1) norm_backward(const NormArgs a)
+__global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? 2 : 1) norm_backward(const NormArgs a)
 {
-    extern __shared__ float4 params[];
+    extern __shared__ uint4 dynamic[];
     __shared__ RowSlots<2> slots[2][THREADS / 64];
     __shared__ float2 peers[2][8];
     __shared__ float merge[THREADS * 8];
@@ -27,23 +21,22 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? NBB : 1) norm_
     const u32 set = blockIdx.x / a.cluster;
     const u64 step = (u64)a.sets * a.groups, step_at = step * a.cols;
     u64 row = (u64)set * a.groups + rg.g, at = row * a.cols + c0;
-    Raw<TYPE, ALIGNED> ry[NV], rh[NV], ri[NV];
-    clear(ry);
-    clear(rh);
-    clear(ri);
+    const bool more = a.dh_in != nullptr;
+    constexpr int STAGES = norm_stages(NV, THREADS);
+    const Ring<TYPE, ALIGNED, NV, THREADS, STAGES> ring = {dynamic + threadIdx.x, more ? 3u : 2u};
+    float4 *params = reinterpret_cast<float4 *>(ring.end());
     float next_mean = 0.f, next_rstd = 0.f;
+    u32 turn = 0;
     auto fetch_row = [&](u64 r, u64 r_at) {
         const u32 end = r < a.rows ? cols : 0u;
         if (r < a.rows) next_mean = a.mean[r], next_rstd = a.rstd[r];
-#pragma unroll
-        for (int k = 0; k < NV; k++) {
-            fetch<TYPE, ALIGNED>(ry[k], a.dy, r_at, c + 256 * k, end);
-            fetch<TYPE, ALIGNED>(rh[k], a.x, r_at, c + 256 * k, end);
-            if (a.dh_in) fetch<TYPE, ALIGNED>(ri[k], a.dh_in, r_at, c + 256 * k, end);
-        }
+        ring.copy(ring.place(turn, 0), a.dy, r_at, c, end);
+        ring.copy(ring.place(turn, 1), a.x, r_at, c, end);
+        if (more) ring.copy(ring.place(turn, 2), a.dh_in, r_at, c, end);
+        copies_commit();
     };
-    constexpr bool PREFETCH = PREB;
-    if (PREFETCH) fetch_row(row, at);
+    ring.clear(c, cols);
+    fetch_row(row, at);
     const void *wp = a.weight ? static_cast<const unsigned char *>(a.weight) + (u64)c0 * type_size(a.param_type) : nullptr;
     float w1[8], dw[NV][8], db[NV][8];
     const u32 plane = a.tpr * NV;               // blocks of the row's threads
@@ -69,21 +62,22 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? NBB : 1) norm_
     u32 parity = 0;
 #pragma unroll 1
     for (; row < a.rows; row += step, at += step_at, parity ^= 1u) {
-        if (!PREFETCH) fetch_row(row, at);
-        float g[NV][8], xh[NV][8], in[NV][8];
         const float mean = next_mean, rstd = next_rstd;
+        turn ^= 1u;
+        if (STAGES == 2) fetch_row(row + step, at + step_at);   // the next row is on its way while this one is worked on
+        ring.wait();
+        const uint4 *py = ring.place(turn ^ 1u, 0), *ph = ring.place(turn ^ 1u, 1), *pi = ring.place(turn ^ 1u, 2);
+        float g[NV][8], xh[NV][8];
         float2 s1 = make_float2(0.f, 0.f), s2 = make_float2(0.f, 0.f);
 #pragma unroll
         for (int k = 0; k < NV; k++) {
-            unpack<TYPE, ALIGNED>(ry[k], at, g[k]);
-            unpack<TYPE, ALIGNED>(rh[k], at, xh[k]);
-            if (a.dh_in) unpack<TYPE, ALIGNED>(ri[k], at, in[k]);
+            unpack<TYPE, ALIGNED>(ring.take(py, k), at, g[k]);
+            unpack<TYPE, ALIGNED>(ring.take(ph, k), at, xh[k]);
             if constexpr (!ALIGNED) {           // (blocks of an ALIGNED row are whole or hold zeros)
                 mask_from(g[k], c + 256 * k, cols, 0.f);
                 mask_from(xh[k], c + 256 * k, cols, 0.f);
             }
         }
-        if (PREFETCH) fetch_row(row + step, at + step_at);      // the next row is on its way while this one is worked on
 #pragma unroll
         for (int k = 0; k < NV; k++) {
             add8(xh[k], -mean);                 // (beyond the row's end g is 0, so that xhat does not matter)
@@ -121,9 +115,11 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? NBB : 1) norm_
             add8(g[k], m1);
 #pragma unroll
             for (int e = 0; e < 8; e += 2) fma2(g[k][e], g[k][e + 1], xh[k][e], xh[k][e + 1], m2, m2, g[k][e], g[k][e + 1]);
-            if (a.dh_in) {
+            if (more) {
+                float in[8];
+                unpack<TYPE, ALIGNED>(ring.take(pi, k), at, in);
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) fma2(g[k][e], g[k][e + 1], g[k][e], g[k][e + 1], rstd, rstd, in[k][e], in[k][e + 1]);
+                for (int e = 0; e < 8; e += 2) fma2(g[k][e], g[k][e + 1], g[k][e], g[k][e + 1], rstd, rstd, in[e], in[e + 1]);
             } else {
                 mul8(g[k], rstd);
             }
@@ -135,6 +131,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? NBB : 1) norm_
             }
             if (a.dx) store_block<TYPE, ALIGNED>(a.dx, at, c + 256 * k, cols, g[k]);
         }
+        if (STAGES == 1) fetch_row(row + step, at + step_at);
     }
     after_kernel_may_start();
     if (!a.partial) return;
@@ -195,7 +192,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) norm_back_sum(const float *par
 
 template <u32 TYPE, bool ALIGNED, int NV, int THREADS> static void launch_drop(const NormArgs &a, cudaStream_t st)
 {
-    const size_t smem = NV == 1 ? 0 : (size_t)a.tpr * NV * 32;
+    const size_t smem = Ring<TYPE, ALIGNED, NV, THREADS, norm_stages(NV, THREADS)>::bytes(a.dh_in ? 3u : 2u) + (NV == 1 ? 0 : (size_t)a.tpr * NV * 32);
     if (a.drop.threshold) launch_norm_kernel(norm_backward<TYPE, ALIGNED, NV, true, THREADS>, a, smem, st);
     else launch_norm_kernel(norm_backward<TYPE, ALIGNED, NV, false, THREADS>, a, smem, st);
 }
@@ -215,7 +212,7 @@ template <u32 TYPE> static void launch_type(const NormArgs &a, cudaStream_t st)
 
 int launch_norm_back(NormArgs &a, u32 type, cudaStream_t st)
 {
-    norm_split(a, true);
+    norm_split(a, kNormBackBlocks);
     if (!a.dweight && !a.dbias) a.partial = nullptr;
     if (a.rows) {
         if (type == ADACOMP_TYPE_F32) launch_type<ADACOMP_TYPE_F32>(a, st);

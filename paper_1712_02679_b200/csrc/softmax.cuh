@@ -9,6 +9,9 @@ namespace cg = cooperative_groups;
 
 constexpr int kSoftThreads = 512;            // most threads of a CTA
 constexpr int kSoftShort = 128;              // threads of a CTA whose rows are one warp each
+// Reach up to which the backward pass keeps its sums by distance in shared memory: with more, 16 warps' lines, the rows on
+// their way and the bias would not fit beside one another, and the lines lie behind the CTAs' sums in the workspace.
+constexpr u32 kLineReach = 200;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // 2^x by the hardware's approximation (PTX ex2.approx: within 2 units in the last place); -inf gives 0.
@@ -19,19 +22,21 @@ __device__ inline float exp2_fast(float x)
     return y;
 }
 
-// v = e^(v - about), about not -inf.  The product with log2(e) is taken of the difference where that of `about` would
+// v = e^(v - about) in the first L blocks, about not -inf.  The product with log2(e) is taken of the difference where that of `about` would
 // overflow: rows of a type's lowest value (a mask added by the caller) keep their softmax.
-template <int NV> __device__ inline void exp_about(float (&v)[NV][8], float about)
+template <int L, int NV> __device__ inline void exp_about(float (&v)[NV][8], float about)
 {
     if (fabsf(about) < 1e38f) {
-        const float about2 = about * kLog2e;
+        const float about2 = -about * kLog2e;
 #pragma unroll
-        for (int k = 0; k < NV; k++)
+        for (int k = 0; k < L; k++) {
+            fma8(v[k], kLog2e, about2);
 #pragma unroll
-            for (int e = 0; e < 8; e++) v[k][e] = exp2_fast(fmaf(v[k][e], kLog2e, -about2));
+            for (int e = 0; e < 8; e++) v[k][e] = exp2_fast(v[k][e]);
+        }
     } else {
 #pragma unroll
-        for (int k = 0; k < NV; k++)
+        for (int k = 0; k < L; k++)
 #pragma unroll
             for (int e = 0; e < 8; e++) v[k][e] = exp2_fast((v[k][e] - about) * kLog2e);
     }
@@ -71,8 +76,39 @@ __device__ inline void add_bias(float (&v)[8], const float *bias, int reach, flo
     const u32 i = (u32)(max(-reach - 8, min(reach, d)) + reach + 8), s = i & 3u;
     const float4 *p = reinterpret_cast<const float4 *>(bias + s * bias_entries((u32)reach) + (i - s));
     const float4 x = p[0], y = p[1];
-    v[0] = fmaf(v[0], scale, x.x), v[1] = fmaf(v[1], scale, x.y), v[2] = fmaf(v[2], scale, x.z), v[3] = fmaf(v[3], scale, x.w);
-    v[4] = fmaf(v[4], scale, y.x), v[5] = fmaf(v[5], scale, y.y), v[6] = fmaf(v[6], scale, y.z), v[7] = fmaf(v[7], scale, y.w);
+    fma2(v[0], v[1], v[0], v[1], scale, scale, x.x, x.y);
+    fma2(v[2], v[3], v[2], v[3], scale, scale, x.z, x.w);
+    fma2(v[4], v[5], v[4], v[5], scale, scale, y.x, y.y);
+    fma2(v[6], v[7], v[6], v[7], scale, scale, y.z, y.w);
+}
+
+// Elements of the first L blocks that dropout drops become 0; blocks go through the generator two by two.
+template <int L, int NV> __device__ inline void drop_row(const Drop &d, u32 row, u32 group0, float (&v)[NV][8])
+{
+#pragma unroll
+    for (int k0 = 0; k0 < L; k0 += 2) {
+        u32 rows[2], groups[2], bits[2][4];
+        rows[0] = rows[1] = row;
+        groups[0] = group0 + 32 * k0;
+        groups[1] = groups[0] + 32;
+        drop_words<2>(d, rows, groups, bits);       // (an odd last block: the other half is dead code)
+#pragma unroll
+        for (int k = 0; k < 2; k++)
+            if (k0 + k < L)
+#pragma unroll
+                for (int e = 0; e < 8; e++) v[k0 + k][e] = dropped(d, bits[k], e) ? 0.f : v[k0 + k][e];
+    }
+}
+
+// f(L) for L = live as a compile-time number (0 counts as 1): the blocks of a row are worked on together, and those that
+// hold nothing not at all.
+template <int L> struct Blocks { static constexpr int value = L; };
+template <int NV, typename F> __device__ inline void with_blocks(int live, F f)
+{
+    if (NV > 3 && live > 3) f(Blocks<NV>());
+    else if (NV > 2 && live > 2) f(Blocks<(NV > 2 ? 3 : NV)>());
+    else if (NV > 1 && live > 1) f(Blocks<(NV > 1 ? 2 : NV)>());
+    else f(Blocks<1>());
 }
 
 // A CTA works on one head of one sequence, on `groups` runs of `run` rows that follow one another.
@@ -92,6 +128,9 @@ struct SoftmaxRows {
         bound = (int)a.k_len;
         if (a.key_len) bound = max(0, min(bound, a.key_len[bh / a.heads]));
     }
+    // How many of a warp's blocks, the first at column c (of lane 0), hold a column before `end`: what lies behind it costs
+    // nothing but its zeros.
+    template <int NV> __device__ static u32 live(u32 end, u32 c) { return end > c ? min((u32)NV, (end - c + 255u) / 256u) : 0u; }
     // one past the last kept column of row i, counted from this CTA's first
     __device__ u32 end(const SoftmaxArgs &a, u32 i) const
     {

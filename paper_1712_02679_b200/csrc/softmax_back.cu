@@ -2,7 +2,7 @@
 #include "softmax.cuh"
 
 #ifndef SBB
-#define SBB 1
+#define SBB 3
 #endif
 namespace adacomp_impl {
 
@@ -16,39 +16,42 @@ namespace adacomp_impl {
 // memory (distances within `reach`) or into one of two registers (beyond it, where the bucket is the side's last).  No
 // addition is atomic, so the order is fixed.  The CTA's warps are added and leave as one sum per bucket;
 // softmax_back_sum adds the CTAs'.
+// Rows that are copied ahead (see Ring): rows beyond 65536 keys leave no room for a second one.
+__host__ __device__ constexpr int soft_back_stages(int nv, int threads) { return nv == 4 && threads == kSoftThreads ? 1 : 2; }
+
 template <u32 TYPE, bool ALIGNED, int NV, bool DROP, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SBB : 1) softmax_backward(const SoftmaxArgs a)
 {
-    extern __shared__ float4 tables[];
+    extern __shared__ uint4 dynamic[];
     __shared__ float part[2][THREADS / 32];
     __shared__ float2 ends[THREADS / 32];
     __shared__ float peers[2][8];
     const RowGroup rg(a.tpr);
     const SoftmaxRows rows(a, rg);
-    if (a.cluster > 1) cg::this_cluster().sync();      // every CTA of the cluster runs before its memory is written
+    const u32 c = block_column<NV>(0, rg.t);                // block k starts at c + 256 k
     const int reach = (int)a.reach;
     const u32 line = 2 * a.reach + 1, cta_warp = threadIdx.x >> 5, cta_warps = blockDim.x >> 5;
-    float *bias = reinterpret_cast<float *>(tables), *all_sums = bias + bias_floats(a.reach);
+    constexpr int STAGES = soft_back_stages(NV, THREADS);
+    const Ring<TYPE, ALIGNED, NV, THREADS, STAGES> ring = {dynamic + threadIdx.x, 2u};
+    float *bias = reinterpret_cast<float *>(ring.end()), *all_sums = bias + bias_floats(a.reach);
+    if (a.reach > kLineReach) all_sums = a.partial + (u64)gridDim.x * a.buckets + (u64)blockIdx.x * cta_warps * line;
     float *sums = all_sums + cta_warp * line;          // entry d + reach; those of -reach and reach stay 0
-    Raw<TYPE, ALIGNED> rs[NV], rd[NV];
-    clear(rs);
-    clear(rd);
     float next_lse = -INFINITY;
+    u32 turn = 0;
     auto fetch_row = [&](u32 i) {
         const u64 row = (u64)rows.bh * a.q_len + i, at = row * a.ld + rows.c0;
         const u32 end = i < rows.i1 ? rows.end(a, i) : 0u;
         if (i < rows.i1) next_lse = a.lse[row];
-#pragma unroll
-        for (int k = 0; k < NV; k++) {
-            const u32 c = block_column<NV>(k, rg.t);
-            fetch<TYPE, ALIGNED>(rs[k], a.scores, at, c, end);
-            fetch<TYPE, ALIGNED>(rd[k], a.dprobs, at, c, end);
-        }
+        ring.copy(ring.place(turn, 0), a.scores, at, c, end);
+        ring.copy(ring.place(turn, 1), a.dprobs, at, c, end);
+        copies_commit();
     };
     fetch_row(rows.i0);
     build_bias(a, rows.bh % a.heads, bias);
-    for (u32 i = rg.lane; i < line; i += 32) sums[i] = 0.f;
+    if (a.partial)
+        for (u32 i = rg.lane; i < line; i += 32) sums[i] = 0.f;
     __syncthreads();
+    if (a.cluster > 1) cg::this_cluster().sync();      // every CTA of the cluster runs before its memory is written
     Drop d;
     if constexpr (DROP) d = drop_begin(a.drop);
     float acc[NV][8];
@@ -88,41 +91,35 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SBB : 1) soft
         const float lse = next_lse;
         const u32 end = lse == -INFINITY ? 0u : rows.end(a, i);
         const int pos = (int)i + a.q_offset;
+        turn ^= 1u;
+        if (STAGES == 2) fetch_row(i + 1);      // the next row is on its way while this one is worked on
+        ring.wait();
+        const int live = rows.live<NV>(end, c - 8 * rg.lane);
+        const uint4 *ps = ring.place(turn ^ 1u, 0), *pd = ring.place(turn ^ 1u, 1);
         float p[NV][8], g[NV][8];
+        float dot;
+        with_blocks<NV>(live, [&](auto blocks) {
+            constexpr int L = decltype(blocks)::value;
 #pragma unroll
-        for (int k = 0; k < NV; k++) {
-            const u32 c = block_column<NV>(k, rg.t);
-            unpack<TYPE, ALIGNED>(rs[k], at, p[k]);
-            unpack<TYPE, ALIGNED>(rd[k], at, g[k]);
-            add_bias(p[k], bias, reach, a.scale, (int)(rows.c0 + c) - pos);
-            mask_from(p[k], c, end, -INFINITY);
-            mask_from(g[k], c, end, 0.f);
-        }
-        fetch_row(i + 1);               // the next row is on its way while this one is worked on
-        if constexpr (DROP) {           // (the factor comes with dot, and where dp is used)
-            constexpr int N = NV < 2 ? 1 : 2;       // blocks that draw together
-#pragma unroll
-            for (int k0 = 0; k0 < NV; k0 += N) {
-                u32 rws[N], groups[N], bits[N][4];
-#pragma unroll
-                for (int k = 0; k < N; k++) rws[k] = (u32)row, groups[k] = (rows.c0 + block_column<NV>(k0 + k, rg.t)) >> 3;
-                drop_words<N>(d, rws, groups, bits);
-#pragma unroll
-                for (int k = 0; k < N; k++)
-#pragma unroll
-                    for (int e = 0; e < 8; e++) g[k0 + k][e] = dropped(d, bits[k], e) ? 0.f : g[k0 + k][e];
+            for (int k = 0; k < L; k++) {
+                unpack<TYPE, ALIGNED>(ring.take(ps, k), at, p[k]);
+                unpack<TYPE, ALIGNED>(ring.take(pd, k), at, g[k]);
+                add_bias(p[k], bias, reach, a.scale, (int)(rows.c0 + c + 256 * k) - pos);
+                mask_from(p[k], c + 256 * k, end, -INFINITY);
+                mask_from(g[k], c + 256 * k, end, 0.f);
             }
-        }
-        exp_about<NV>(p, lse == -INFINITY ? 0.f : lse);
-        float dot = 0.f, dot2 = 0.f;
+            if constexpr (DROP) drop_row<L>(d, (u32)row, (rows.c0 + c) >> 3, g);      // (the factor comes where dp is used)
+            exp_about<L>(p, lse == -INFINITY ? 0.f : lse);
+            float2 dots = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int k = 0; k < NV; k++)
+            for (int k = 0; k < L; k++) dot8(dots, p[k], g[k]);
+            dot = dots.x + dots.y;
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                dot = fmaf(p[k][e], g[k][e], dot);
-                dot2 = fmaf(p[k][e + 1], g[k][e + 1], dot2);
-            }
-        dot += dot2;
+            for (int k = L; k < NV; k++)
+#pragma unroll
+                for (int e = 0; e < 8; e++) p[k][e] = 0.f;
+        });
+        if (STAGES == 1) fetch_row(i + 1);
         // A sum's logarithm does not show beside a statistic this large (ulp 2^-9 and up): P is then normalised again.
         // (A property of the row, so that all its threads meet in row_sum.)
         if (lse != -INFINITY && fabsf(lse) > 16384.f) {
@@ -142,21 +139,34 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SBB : 1) soft
         const float factor = DROP ? d.factor : 1.f;
         dot = row_sum(dot) * factor;
         float carry = 0.f;              // lane 0: the last sum of the block before
+        with_blocks<NV>(live, [&](auto blocks) {
+            constexpr int L = decltype(blocks)::value;
 #pragma unroll
-        for (int k = 0; k < NV; k++) {
+            for (int k = 0; k < L; k++) {
 #pragma unroll
-            for (int e = 0; e < 8; e++) p[k][e] *= DROP ? fmaf(g[k][e], factor, -dot) : g[k][e] - dot;
+                for (int e = 0; e < 8; e += 2) {
+                    if (DROP) fma2(g[k][e], g[k][e + 1], g[k][e], g[k][e + 1], factor, factor, -dot, -dot);
+                    else add2(g[k][e], g[k][e + 1], g[k][e], g[k][e + 1], -dot, -dot);
+                }
+                mul8(p[k], g[k]);
+            }
             if (a.partial) {
-                const float from = __shfl_sync(kAllLanes, acc[k][7], (rg.lane + 31u) & 31u);
 #pragma unroll
-                for (int e = 7; e > 0; e--) acc[k][e] = acc[k][e - 1] + p[k][e];
-                acc[k][0] = (rg.lane ? from : carry) + p[k][0];
-                carry = from;
+                for (int k = 0; k < NV; k++) {
+                    const float from = __shfl_sync(kAllLanes, acc[k][7], (rg.lane + 31u) & 31u);
+#pragma unroll
+                    for (int e = 7; e > 0; e--) acc[k][e] = k < L ? acc[k][e - 1] + p[k][e] : acc[k][e - 1];
+                    acc[k][0] = rg.lane ? from : carry;
+                    if (k < L) acc[k][0] += p[k][0];
+                    carry = from;
+                }
             }
 #pragma unroll
-            for (int e = 0; e < 8; e++) p[k][e] *= a.scale;
-            store_block<TYPE, ALIGNED>(a.dscores, at, block_column<NV>(k, rg.t), rows.cols, p[k]);
-        }
+            for (int k = 0; k < NV; k++) {
+                if (k < L) mul8(p[k], a.scale);
+                store_block<TYPE, ALIGNED>(a.dscores, at, c + 256 * k, rows.cols, p[k]);
+            }
+        });
         if (a.partial && rg.lane == 0 && i > rows.i0) put(last_col - (pos - 1), carry);
     }
     if (!a.partial) return;
@@ -166,7 +176,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SBB : 1) soft
 #pragma unroll
         for (int k = 0; k < NV; k++)
 #pragma unroll
-            for (int e = 0; e < 8; e++) put((int)(rows.c0 + block_column<NV>(k, rg.t)) + e - pos, acc[k][e]);
+            for (int e = 0; e < 8; e++) put((int)(rows.c0 + c + 256 * k) + e - pos, acc[k][e]);
     }
     after_kernel_may_start();
     before = warp_sum(before);
@@ -230,14 +240,15 @@ softmax_back_sum(const float *partial, float *dtable, u32 batch, u32 heads, u32 
 
 template <u32 TYPE, bool ALIGNED, int NV, int THREADS> static void launch_drop(const SoftmaxArgs &a, cudaStream_t st)
 {
-    const size_t smem = (bias_floats(a.reach) + (size_t)(a.tpr * a.groups / 32) * (2 * a.reach + 1)) * sizeof(float);
+    const size_t smem = Ring<TYPE, ALIGNED, NV, THREADS, soft_back_stages(NV, THREADS)>::bytes(2) + 
+                        (bias_floats(a.reach) + (a.reach > kLineReach ? 0 : (size_t)(a.tpr * a.groups / 32) * (2 * a.reach + 1))) * sizeof(float);
     if (a.drop.threshold) launch_softmax_kernel(softmax_backward<TYPE, ALIGNED, NV, true, THREADS>, a, smem, st);
     else launch_softmax_kernel(softmax_backward<TYPE, ALIGNED, NV, false, THREADS>, a, smem, st);
 }
 
 template <u32 TYPE, bool ALIGNED> static void launch_blocks(const SoftmaxArgs &a, cudaStream_t st)
 {
-    if (a.tpr == 32) {
+    if (a.threads == kSoftShort) {
         if (a.per == 1) launch_drop<TYPE, ALIGNED, 1, kSoftShort>(a, st);
         else if (a.per == 2) launch_drop<TYPE, ALIGNED, 2, kSoftShort>(a, st);
         else launch_drop<TYPE, ALIGNED, 4, kSoftShort>(a, st);
@@ -253,9 +264,23 @@ template <u32 TYPE> static void launch_type(const SoftmaxArgs &a, cudaStream_t s
     else launch_blocks<TYPE, false>(a, st);
 }
 
+// Sums by bucket of every CTA, and sums by distance of every warp where those do not fit into shared memory.
+size_t softmax_workspace(SoftmaxArgs &a)
+{
+    size_t most = 0;
+    for (int aligned = 0; aligned < 2; aligned++) {
+        softmax_split(a, true, aligned != 0);
+        const size_t ctas = (size_t)a.batch * a.heads * a.chunks * a.cluster;
+        const size_t lines = a.reach > kLineReach ? ctas * (a.tpr * a.groups / 32) * (2 * a.reach + 1) : 0;
+        const size_t bytes = (ctas * a.buckets + lines) * sizeof(float);
+        if (bytes > most) most = bytes;
+    }
+    return most;
+}
+
 int launch_softmax_back(SoftmaxArgs &a, u32 type, cudaStream_t st)
 {
-    softmax_split(a);
+    softmax_split(a, true, a.ld % 8u == 0);
     if (!a.table || !a.dtable) a.partial = nullptr;
     const bool any = (u64)a.batch * a.heads * a.q_len != 0;
     if (any) {
