@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import List, Optional, Sequence
 
 import torch
@@ -164,16 +165,16 @@ def lib() -> C.CDLL:
         L.adacomp_device_status_reset.restype = C.c_int
         L.adacomp_device_status_reset.argtypes = [C.c_void_p]
         vp, u64, u32 = C.c_void_p, C.c_uint64, C.c_uint32
-        norm, soft, rel = C.POINTER(adacomp_norm_options), C.POINTER(adacomp_softmax_options), C.POINTER(adacomp_relpos)
+        rel = C.POINTER(adacomp_relpos)         # (the option structures go as bytes, see _pack_norm)
         for name, restype, argtypes in [
                 ("adacomp_dropout", C.c_int, [vp, vp, u64, u32, u32, C.c_float, vp, u32, vp]),
-                ("adacomp_layer_norm", C.c_int, [vp] * 8 + [norm, vp]),
+                ("adacomp_layer_norm", C.c_int, [vp] * 10),
                 ("adacomp_layer_norm_workspace", C.c_size_t, [u64, u32]),
-                ("adacomp_layer_norm_backward", C.c_int, [vp] * 11 + [C.c_size_t, norm, vp]),
+                ("adacomp_layer_norm_backward", C.c_int, [vp] * 11 + [C.c_size_t, vp, vp]),
                 ("adacomp_relpos_plan", C.c_int, [u32, u32, u32, rel]),
-                ("adacomp_bias_softmax", C.c_int, [vp, vp, rel, vp, vp, soft, vp]),
+                ("adacomp_bias_softmax", C.c_int, [vp, vp, rel, vp, vp, vp, vp]),
                 ("adacomp_bias_softmax_workspace", C.c_size_t, [u32, u32, u32, u32, rel]),
-                ("adacomp_bias_softmax_backward", C.c_int, [vp, vp, vp, rel, vp, vp, vp, vp, C.c_size_t, soft, vp])]:
+                ("adacomp_bias_softmax_backward", C.c_int, [vp, vp, vp, rel, vp, vp, vp, vp, C.c_size_t, vp, vp])]:
             f = getattr(L, name)
             f.restype, f.argtypes = restype, argtypes
         _lib = L
@@ -574,19 +575,24 @@ def _type_of(t: torch.Tensor, what: str) -> int:
 
 
 def _like(t: Optional[torch.Tensor], what: str, shape, dtype) -> Optional[int]:
-    """Pointer of a dense CUDA tensor of this shape (a torch.Size or a tuple) and type (None: NULL)."""
+    """Pointer of a dense CUDA tensor of this shape and type (None: NULL)."""
     if t is None:
         return None
+    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
     if t.shape != shape:
         raise ValueError(f"{what} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-    if t.is_cuda and t.dtype is dtype and t.is_contiguous():
-        return t.data_ptr()
-    return _dev_ptr(t, what, dtype)         # says what is wrong
+    return _dev_ptr(t, what, dtype)         # says what else is wrong
 
 
 def _rng_ptr(rng: Optional[torch.Tensor]) -> Optional[int]:
     """rng: int64[2] CUDA tensor {seed, step}."""
-    return None if rng is None else _like(rng, "rng", (2,), torch.int64)
+    return _like(rng, "rng", (2,), torch.int64)
+
+
+def _stream_of(t: torch.Tensor, stream) -> Optional[int]:
+    """As _stream, for a call on the CUDA tensor t: without a Stream object, which costs as much as the call."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else _stream(stream)
 
 
 def _rows_cols(x: torch.Tensor, what: str):
@@ -596,26 +602,35 @@ def _rows_cols(x: torch.Tensor, what: str):
     return (x.numel() // cols if cols else 0), cols
 
 
-def adacomp_dropout(x, y, p: float, rng, site: int = 0, stream=None) -> None:
-    """y = dropout(x), rows being all dimensions but the last; the backward pass is the same call on dy."""
-    rows, cols = _rows_cols(x, "x")
-    shape, dtype = x.shape, x.dtype
-    _check(lib().adacomp_dropout(_dev_ptr(x, "x"), _like(y, "y", shape, dtype), rows, cols, _type_of(x, "x"), p,
-                                 _rng_ptr(rng), site, _stream(stream)), "adacomp_dropout")
-
-
-def _param_type(params, what: str) -> int:
+def _param_dtype(params, what: str):
+    """The one dtype of the tensors that are there, float32 when none is."""
     kind = None
     for t in params:
         if t is not None:
-            if kind is not None and t.dtype is not kind:
+            if kind is None:
+                kind = t.dtype
+            elif t.dtype is not kind:
                 raise ValueError(f"{what} must have one dtype")
-            kind = t.dtype
     if kind is None:
-        return ADACOMP_TYPE_F32
+        return torch.float32
     if kind not in _TYPES:
         raise ValueError(f"{what} must be float32, bfloat16 or float16")
-    return _TYPES[kind]
+    return kind
+
+
+def adacomp_dropout(x, y, p: float, rng, site: int = 0, stream=None) -> None:
+    """y = dropout(x), rows being all dimensions but the last; the backward pass is the same call on dy."""
+    rows, cols = _rows_cols(x, "x")
+    dtype = x.dtype
+    rc = (_lib or lib()).adacomp_dropout(_dev_ptr(x, "x"), _like(y, "y", x.shape, dtype), rows, cols, _type_of(x, "x"), p,
+                                         _rng_ptr(rng), site, _stream_of(x, stream))
+    if rc:
+        _check(rc, "adacomp_dropout")
+
+
+# (the option structures as bytes: making a ctypes structure costs more than the call)
+_pack_norm = struct.Struct("QIIIffIN").pack
+_pack_softmax = struct.Struct("IIIIQIfIiNfIN").pack
 
 
 def adacomp_layer_norm(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-5, residual=None, h_out=None,
@@ -623,15 +638,15 @@ def adacomp_layer_norm(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e
     """h = residual + dropout(x); y = layer_norm(h) * weight + bias over the last dimension.  mean, rstd: float32, one
     per row, for the backward call."""
     rows, cols = _rows_cols(x, "x")
-    kind = _param_type((weight, bias), "weight and bias")
-    opt = adacomp_norm_options(rows, cols, _type_of(x, "x"), kind, eps, p, site, _rng_ptr(rng))
     shape, dtype, vec, f32 = x.shape, x.dtype, (cols,), torch.float32
-    stat = shape[:-1]
-    param = _DTYPES[kind]
-    _check(lib().adacomp_layer_norm(
+    param, stat = _param_dtype((weight, bias), "weight and bias"), shape[:-1]
+    opt = _pack_norm(rows, cols, _type_of(x, "x"), _TYPES[param], eps, p, site, (_rng_ptr(rng) or 0) if p else 0)
+    rc = (_lib or lib()).adacomp_layer_norm(
         _dev_ptr(x, "x"), _like(residual, "residual", shape, dtype), _like(weight, "weight", vec, param),
         _like(bias, "bias", vec, param), _like(h_out, "h_out", shape, dtype), _like(y, "y", shape, dtype),
-        _like(mean, "mean", stat, f32), _like(rstd, "rstd", stat, f32), opt, _stream(stream)), "adacomp_layer_norm")
+        _like(mean, "mean", stat, f32), _like(rstd, "rstd", stat, f32), opt, _stream_of(x, stream))
+    if rc:
+        _check(rc, "adacomp_layer_norm")
 
 
 def adacomp_layer_norm_workspace(rows: int, cols: int) -> int:
@@ -643,17 +658,17 @@ def adacomp_layer_norm_backward(dy, h, weight, mean, rstd, dx, dweight=None, dbi
                                 dresidual=None, p: float = 0.0, rng=None, site: int = 0, stream=None) -> None:
     """Gradients of adacomp_layer_norm; any output may be None.  dh_in: the gradient reaching h from elsewhere."""
     rows, cols = _rows_cols(h, "h")
-    kind = _param_type((weight, dweight, dbias), "weight, dweight and dbias")
-    opt = adacomp_norm_options(rows, cols, _type_of(h, "h"), kind, 0.0, p, site, _rng_ptr(rng))
     shape, dtype, vec, f32 = h.shape, h.dtype, (cols,), torch.float32
-    stat = shape[:-1]
-    param = _DTYPES[kind]
-    _check(lib().adacomp_layer_norm_backward(
+    param, stat = _param_dtype((weight, dweight, dbias), "weight, dweight and dbias"), shape[:-1]
+    opt = _pack_norm(rows, cols, _type_of(h, "h"), _TYPES[param], 0.0, p, site, (_rng_ptr(rng) or 0) if p else 0)
+    rc = (_lib or lib()).adacomp_layer_norm_backward(
         _like(dy, "dy", shape, dtype), _like(dh_in, "dh_in", shape, dtype), _dev_ptr(h, "h"),
         _like(weight, "weight", vec, param), _like(mean, "mean", stat, f32), _like(rstd, "rstd", stat, f32),
         _like(dx, "dx", shape, dtype), _like(dresidual, "dresidual", shape, dtype), _like(dweight, "dweight", vec, param),
         _like(dbias, "dbias", vec, param), _dev_ptr(workspace, "workspace", torch.uint8),
-        workspace.numel() if workspace is not None else 0, opt, _stream(stream)), "adacomp_layer_norm_backward")
+        workspace.numel() if workspace is not None else 0, opt, _stream_of(h, stream))
+    if rc:
+        _check(rc, "adacomp_layer_norm_backward")
 
 
 def adacomp_relpos_plan(num_buckets: int, max_distance: int, bidirectional: bool = True) -> adacomp_relpos:
@@ -702,9 +717,8 @@ def _softmax_call(scores, table, relpos, others, scale, causal, q_offset, key_le
         if relpos is None:
             raise ValueError("a bias table needs its buckets (adacomp_relpos_plan)")
         tp, rel = _like(table, "table", (relpos.num_buckets, h), torch.float32), relpos
-    opt = adacomp_softmax_options(b, h, q, k, ld if ld is not None else k, _type_of(scores, "scores"), scale,
-                                  1 if causal else 0, q_offset, _like(key_len, "key_len", (b,), torch.int32), p, site,
-                                  _rng_ptr(rng))
+    opt = _pack_softmax(b, h, q, k, ld if ld is not None else k, _type_of(scores, "scores"), scale, 1 if causal else 0,
+                        q_offset, _like(key_len, "key_len", (b,), torch.int32) or 0, p, site, (_rng_ptr(rng) or 0) if p else 0)
     return opt, tp, rel
 
 
@@ -712,10 +726,12 @@ def adacomp_bias_softmax(scores, table, relpos: Optional[adacomp_relpos], probs,
                          causal: bool = False, q_offset: int = 0, key_len=None, p: float = 0.0, rng=None, site: int = 0,
                          stream=None) -> None:
     """probs = dropout(softmax(scale * scores + bias)) over [batch, heads, queries, keys]; rows may be spaced apart."""
-    opt, tp, rel = _softmax_call(scores, table, relpos, [(probs, "probs")], scale, causal, q_offset, key_len, p, rng, site)
-    _check(lib().adacomp_bias_softmax(scores.data_ptr(), tp, rel, probs.data_ptr(),
-                                      _like(lse, "lse", scores.shape[:3], torch.float32), opt, _stream(stream)),
-           "adacomp_bias_softmax")
+    opt, tp, rel = _softmax_call(scores, table, relpos, ((probs, "probs"),), scale, causal, q_offset, key_len, p, rng, site)
+    rc = (_lib or lib()).adacomp_bias_softmax(scores.data_ptr(), tp, rel, probs.data_ptr(),
+                                              _like(lse, "lse", scores.shape[:3], torch.float32), opt,
+                                              _stream_of(scores, stream))
+    if rc:
+        _check(rc, "adacomp_bias_softmax")
 
 
 def adacomp_bias_softmax_workspace(batch: int, heads: int, q_len: int, k_len: int, relpos: adacomp_relpos) -> int:
@@ -727,10 +743,12 @@ def adacomp_bias_softmax_backward(dprobs, scores, table, relpos: Optional[adacom
                                   workspace=None, scale: float = 1.0, causal: bool = False, q_offset: int = 0, key_len=None,
                                   p: float = 0.0, rng=None, site: int = 0, stream=None) -> None:
     """Gradients of adacomp_bias_softmax: dscores and, unless None, the bias table's."""
-    opt, tp, rel = _softmax_call(scores, table, relpos, [(dprobs, "dprobs"), (dscores, "dscores")], scale, causal, q_offset,
+    opt, tp, rel = _softmax_call(scores, table, relpos, ((dprobs, "dprobs"), (dscores, "dscores")), scale, causal, q_offset,
                                  key_len, p, rng, site)
-    _check(lib().adacomp_bias_softmax_backward(
+    rc = (_lib or lib()).adacomp_bias_softmax_backward(
         dprobs.data_ptr(), scores.data_ptr(), tp, rel, _like(lse, "lse", scores.shape[:3], torch.float32),
         dscores.data_ptr(), _like(dtable, "dtable", table.shape if table is not None else (), torch.float32),
         _dev_ptr(workspace, "workspace", torch.uint8), workspace.numel() if workspace is not None else 0, opt,
-        _stream(stream)), "adacomp_bias_softmax_backward")
+        _stream_of(scores, stream))
+    if rc:
+        _check(rc, "adacomp_bias_softmax_backward")

@@ -69,7 +69,7 @@ static int check_softmax(const float *table, const adacomp_relpos *relpos, const
     a.q_offset = opt->q_offset;
     a.key_len = opt->key_len;
     a.table = table;
-    a.reach = a.both = 0;
+    a.reach = a.both = a.search = 0;
     a.side = a.buckets = 1;
     a.first[0] = 0;
     if (table) {
@@ -86,6 +86,8 @@ static int check_softmax(const float *table, const adacomp_relpos *relpos, const
         a.buckets = relpos->num_buckets;
         a.both = sides == 2u;
         a.reach = a.first[a.side - 1];
+        for (a.search = 1; a.search * 2 < a.side; a.search *= 2) {
+        }
         if (a.reach < 1 || a.reach > ADACOMP_MAX_DISTANCE) return ADACOMP_ERR_SHAPE;
     }
     if ((reinterpret_cast<uintptr_t>(opt->key_len) | reinterpret_cast<uintptr_t>(table)) & 3u) return ADACOMP_ERR_ALIGN;

@@ -214,53 +214,6 @@ __device__ inline void fetch(Raw<TYPE, ALIGNED> &r, const void *base, u64 row_at
     for_chunks<TYPE, ALIGNED>(base, row_at, c, end, [&](int i, const uint4 *p) { r.q[i] = *p; });
 }
 
-// Rows on their way: each thread copies its own chunks of the next rows into its own places of shared memory
-// (cp.async) and reads them back itself, so that nobody waits for anybody, and no register holds what has not arrived.
-// `arrays` tensors, STAGES rows of each: with two, the next row is copied while one is worked on; with one, for the widest
-// rows, only once its places have been read.
-template <u32 TYPE, bool ALIGNED, int NV, int THREADS, int STAGES> struct Ring {
-    static constexpr int kChunks = sizeof(Raw<TYPE, ALIGNED>) / 16;
-    static constexpr u32 kArray = NV * kChunks * THREADS;          // in 16 bytes
-    static constexpr size_t bytes(u32 arrays) { return (size_t)STAGES * arrays * kArray * 16; }
-    uint4 *mine;
-    u32 arrays;
-    __device__ uint4 *place(u32 turn, u32 array) const { return mine + ((turn & (STAGES - 1)) * arrays + array) * kArray; }
-    __device__ uint4 *end() const { return mine - threadIdx.x + STAGES * arrays * kArray; }
-    // What was asked for before the last request has arrived (one stage: the last request itself).
-    __device__ static void wait()
-    {
-        if (STAGES == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
-        else asm volatile("cp.async.wait_group 0;" ::: "memory");
-    }
-    // Blocks k = 0, 1, .. start at columns c + 256 k.
-    __device__ static void copy(uint4 *to, const void *base, u64 row_at, u32 c, u32 end)
-    {
-#pragma unroll
-        for (int k = 0; k < NV; k++)
-            for_chunks<TYPE, ALIGNED>(base, row_at, c + 256 * k, end, [&](int i, const uint4 *p) {
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(to + (k * kChunks + i) * THREADS)), "l"(p)
-                             : "memory");
-            });
-    }
-    __device__ static Raw<TYPE, ALIGNED> take(const uint4 *from, int k)
-    {
-        Raw<TYPE, ALIGNED> r;
-#pragma unroll
-        for (int i = 0; i < kChunks; i++) r.q[i] = from[(k * kChunks + i) * THREADS];
-        return r;
-    }
-    // Places that no copy reaches, where the kernel counts on zeros behind a row's end.
-    __device__ void clear(u32 c, u32 end) const
-    {
-        for (u32 j = 0; j < STAGES * arrays; j++)
-#pragma unroll
-            for (int k = 0; k < NV; k++)
-#pragma unroll
-                for (int i = 0; i < kChunks; i++)
-                    if (c + 256 * k >= end) mine[j * kArray + (k * kChunks + i) * THREADS] = make_uint4(0u, 0u, 0u, 0u);
-    }
-};
-
 __device__ inline void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 
 // w[0..n) = in[shift .. shift + n) for a shift of 0..3 words (the same for the whole warp)
@@ -320,12 +273,13 @@ __device__ inline void store_block(void *base, u64 row_at, u32 c, u32 cols, cons
     constexpr u32 per = chunk_elems<TYPE>();
     const u32 s = ALIGNED ? 0u : (u32)row_at & (per - 1u);
     if (ALIGNED || s == 0u) {
-        if (c + 8 <= cols) {
-            store8<TYPE>(base, row_at + c, narrow8<TYPE>(v));
-        } else if (c < cols) {          // what lies behind the row's last column is not this row's
+        if (c + 8 <= cols) store8<TYPE>(base, row_at + c, narrow8<TYPE>(v));
+        if (cols & 7u) {                // (what lies behind the row's last column is not this row's)
+            if (c < cols && c + 8 > cols) {
 #pragma unroll
-            for (int e = 0; e < 8; e++)
-                if (c + e < cols) store1<TYPE>(base, row_at + c + e, v[e]);
+                for (int e = 0; e < 8; e++)
+                    if (c + e < cols) store1<TYPE>(base, row_at + c + e, v[e]);
+            }
         }
         return;
     }
@@ -369,6 +323,167 @@ __device__ inline void store_block(void *base, u64 row_at, u32 c, u32 cols, cons
         }
     }
 }
+
+// The block whose elements begin `s` elements behind p: lanes read neighbouring blocks of a line in shared memory, from
+// any element on, by 8-byte and 4-byte reads (s is the same for the warp); an odd 16-bit offset shifts by half a word.
+template <u32 TYPE> __device__ inline void read_at(const uint4 *p, u32 s, Vec8<TYPE> &r)
+{
+    constexpr bool WORDS = TYPE == ADACOMP_TYPE_F32;
+    constexpr int N = WORDS ? 8 : 5;
+    const u32 first = WORDS ? s : s >> 1;
+    const u32 *w = reinterpret_cast<const u32 *>(p) + first;
+    u32 x[N + 1];
+    if (first & 1u) {
+        x[0] = w[0];
+#pragma unroll
+        for (int i = 1; i + 1 < N + 1; i += 2) {
+            if (WORDS && i == N - 1) {
+                x[i] = w[i];
+            } else {
+                const uint2 q = *reinterpret_cast<const uint2 *>(w + i);
+                x[i] = q.x, x[i + 1] = q.y;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i + 1 < N; i += 2) {
+            const uint2 q = *reinterpret_cast<const uint2 *>(w + i);
+            x[i] = q.x, x[i + 1] = q.y;
+        }
+        if (!WORDS) x[4] = w[4];
+    }
+    u32 *out = reinterpret_cast<u32 *>(r.q);
+#pragma unroll
+    for (int i = 0; i < (WORDS ? 8 : 4); i++) out[i] = WORDS ? x[i] : __funnelshift_r(x[i], x[i + 1], (s & 1u) * 16u);
+}
+
+// Rows on their way: each thread copies its chunks of the next rows into shared memory (cp.async), so that no register
+// holds what has not arrived and nothing is loaded twice.  ALIGNED rows: a thread reads back what it copied itself, and
+// nobody waits for anybody.  Others: a warp's chunks form a line of its own, in which every block lies shifted by the row's
+// offset; the warp's lanes wait for one another.  On the way out such a row is joined into whole chunks in the same line.
+// `arrays` tensors, STAGES rows of each: with two, the next row is copied while one is worked on; with one, for the widest
+// rows, only once its places have been read.
+template <u32 TYPE, bool ALIGNED, int NV, int THREADS, int STAGES> struct Ring {
+    static constexpr u32 kPer = chunk_elems<TYPE>();
+    static constexpr int kChunks = 8 / kPer;                        // of a block
+    static constexpr u32 kLine = 32 * NV * kChunks + 2;             // a warp's line: one chunk more on either side
+    static constexpr u32 kArray = ALIGNED ? NV * kChunks * THREADS : THREADS / 32 * kLine;      // in 16 bytes
+    static constexpr size_t bytes(u32 arrays) { return (size_t)STAGES * arrays * kArray * 16; }
+    uint4 *base, *mine;     // mine: this thread's first chunk
+    u32 arrays, lane;
+    __device__ Ring(void *smem, u32 n)
+        : base(static_cast<uint4 *>(smem)),
+          mine(base + (ALIGNED ? threadIdx.x : (threadIdx.x >> 5) * kLine + 1 + (threadIdx.x & 31u) * kChunks)), arrays(n),
+          lane(threadIdx.x & 31u)
+    {
+    }
+    __device__ uint4 *place(u32 turn, u32 array) const { return mine + ((turn & (STAGES - 1)) * arrays + array) * kArray; }
+    __device__ void *end() const { return base + STAGES * arrays * kArray; }
+    __device__ static constexpr u32 at(int k, int i) { return ALIGNED ? (k * kChunks + i) * THREADS : k * 32 * kChunks + i; }
+    // Blocks k = 0, 1, .. start at columns c + 256 k of the row at element row_at; columns before `last` are wanted.
+    __device__ void copy(uint4 *to, const void *from, u64 row_at, u32 c, u32 last) const
+    {
+        const u32 s = ALIGNED ? 0u : (u32)row_at & (kPer - 1u);
+        const unsigned char *p = static_cast<const unsigned char *>(from) + (row_at + c - s) * type_size(TYPE);
+        const u32 dst = smem_addr(to);
+#pragma unroll
+        for (int k = 0; k < NV; k++)
+#pragma unroll
+            for (int i = 0; i < kChunks; i++) {
+                const int first = (int)(c + 256 * k + i * kPer) - (int)s;       // a column of this chunk, or below 0
+                copy_if(last > 0u && first < (int)last, dst + at(k, i) * 16, p + (256 * k + i * kPer) * type_size(TYPE));
+            }
+        if (!ALIGNED && s != 0u)
+            copy_if(lane == 31u && c + 256 * (NV - 1) + 8u - s < last, dst + at(NV - 1, kChunks) * 16,
+                    p + (256 * (NV - 1) + 8u) * type_size(TYPE));
+    }
+    __device__ static void copy_if(bool on, u32 dst, const void *p)
+    {
+        asm volatile("{\n\t.reg .pred on;\n\tsetp.ne.u32 on, %2, 0;\n\t@on cp.async.cg.shared.global [%0], [%1], 16;\n\t}" ::"r"(dst),
+                     "l"(p), "r"((u32)on)
+                     : "memory");
+    }
+    // Before copies into places that have been read.
+    __device__ static void release()
+    {
+        if (!ALIGNED) __syncwarp();
+    }
+    // What was asked for before the last request has arrived (one stage: the last request itself).
+    __device__ static void wait()
+    {
+        if (STAGES == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 0;" ::: "memory");
+        if (!ALIGNED) __syncwarp();
+    }
+    // Block k in binary32 (see mask_from for its elements that were not asked for).
+    __device__ static void read(const uint4 *from, int k, u64 row_at, float (&v)[8])
+    {
+        Vec8<TYPE> r;
+        if constexpr (ALIGNED) {
+#pragma unroll
+            for (int i = 0; i < kChunks; i++) r.q[i] = from[at(k, i)];
+        } else {
+            read_at<TYPE>(from + at(k, 0), (u32)row_at & (kPer - 1u), r);
+        }
+        widen8<TYPE>(r, v);
+    }
+    // Places that no copy reaches, where the kernel counts on zeros behind a row's end.
+    __device__ void clear(u32 c, u32 last) const
+    {
+        if (!ALIGNED) return;
+        for (u32 j = 0; j < STAGES * arrays; j++)
+#pragma unroll
+            for (int k = 0; k < NV; k++)
+#pragma unroll
+                for (int i = 0; i < kChunks; i++)
+                    if (c + 256 * k >= last) mine[j * kArray + at(k, i)] = make_uint4(0u, 0u, 0u, 0u);
+    }
+    // Stores the row's columns before `cols`; `line`: places of this thread's row that have been read, which a row that is
+    // not ALIGNED goes through.
+    __device__ void store(void *to, u64 row_at, u32 c, u32 cols, const float (&v)[NV][8], uint4 *line) const
+    {
+        const u32 s = ALIGNED ? 0u : (u32)row_at & (kPer - 1u);
+        if (ALIGNED || s == 0u) {
+#pragma unroll
+            for (int k = 0; k < NV; k++) store_block<TYPE, true>(to, row_at, c + 256 * k, cols, v[k]);
+            return;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+            const Vec8<TYPE> r = narrow8<TYPE>(v[k]);
+#pragma unroll
+            for (int i = 0; i < kChunks; i++) line[at(k, i)] = r.q[i];
+        }
+        __syncwarp();
+        unsigned char *p = static_cast<unsigned char *>(to) + (row_at + c - s) * type_size(TYPE);
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+            // what lies s elements before the block is whole chunks; the warp's first one starts in another warp's columns
+            const u32 ck = c + 256 * k;
+            Vec8<TYPE> r;
+            read_at<TYPE>(line + at(k, 0) - 1, kPer - s, r);
+            const bool inside = k > 0 || lane > 0u;
+            bool whole = true;
+#pragma unroll
+            for (int i = 0; i < kChunks; i++) {
+                const bool full = (i > 0 || inside) && ck + (i + 1) * kPer - s <= cols;
+                if (full) *reinterpret_cast<uint4 *>(p + (256 * k + i * kPer) * type_size(TYPE)) = r.q[i];
+                whole = whole && full;
+            }
+            const bool next = (k + 1 < NV || lane < 31u) && ck + 8u + kPer - s <= cols;     // takes this block's last elements
+            if (!(whole && next)) {
+#pragma unroll
+                for (u32 e = 0; e < 8; e++) {
+                    // element e lies in chunk (e + s) / kPer of the block's chunks, the last of which is the next block's
+                    const u32 chunk = (e + s) / kPer;
+                    const bool done = chunk == (u32)kChunks ? next : (chunk > 0u || inside) && ck + (chunk + 1) * kPer - s <= cols;
+                    if (ck + e < cols && !done) store1<TYPE>(to, row_at + ck + e, v[k][e]);
+                }
+            }
+        }
+    }
+};
 
 // A parameter vector (its type known at run time; it starts on a vector boundary).
 __device__ inline void load_param(const void *p, u32 type, u32 c, u32 cols, float fill, float (&v)[8])

@@ -72,6 +72,7 @@ struct SoftmaxArgs {
     float scale;
     DropArgs drop;
     u32 buckets, side, both, reach;              // the bias: see include/adacomp.h (adacomp_relpos)
+    u32 search;                                  // the largest power of two below `side` (0: none)
     uint16_t first[ADACOMP_MAX_BUCKETS];
 };
 

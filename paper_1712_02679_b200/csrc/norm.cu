@@ -43,13 +43,14 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? 2 : 1) norm_fo
     const u32 c = block_column<NV>(0, rg.t);                // block k starts at c + 256 k
     const bool res = a.residual != nullptr;
     constexpr int STAGES = norm_stages(NV, THREADS);
-    const Ring<TYPE, ALIGNED, NV, THREADS, STAGES> ring = {dynamic + threadIdx.x, res ? 2u : 1u};
+    const Ring<TYPE, ALIGNED, NV, THREADS, STAGES> ring(dynamic, res ? 2u : 1u);
     float4 *params = reinterpret_cast<float4 *>(ring.end());
     const u64 step = (u64)a.sets * a.groups, step_at = step * a.cols;
     u64 row = (u64)(blockIdx.x / a.cluster) * a.groups + rg.g, at = row * a.cols + c0;
     u32 turn = 0;
     auto fetch_row = [&](u64 r, u64 r_at) {
         const u32 end = r < a.rows ? cols : 0u;
+        ring.release();
         ring.copy(ring.place(turn, 0), a.x, r_at, c, end);
         if (res) ring.copy(ring.place(turn, 1), a.residual, r_at, c, end);
         copies_commit();
@@ -99,11 +100,11 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? 2 : 1) norm_fo
         turn ^= 1u;
         if (STAGES == 2) fetch_row(row + step, at + step_at);   // the next row is on its way while this one is worked on
         ring.wait();
-        const uint4 *px = ring.place(turn ^ 1u, 0), *pr = ring.place(turn ^ 1u, 1);
+        uint4 *px = ring.place(turn ^ 1u, 0), *pr = ring.place(turn ^ 1u, 1);
         float h[NV][8];
 #pragma unroll
         for (int k = 0; k < NV; k++) {
-            unpack<TYPE, ALIGNED>(ring.take(px, k), at, h[k]);
+            ring.read(px, k, at, h[k]);
             if constexpr (DROP) {
                 u32 bits[4];
                 drop_words(d, (u32)row, (c0 + c + 256 * k) >> 3, bits);
@@ -111,16 +112,19 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? 2 : 1) norm_fo
             }
             if (res) {
                 float r[8];
-                unpack<TYPE, ALIGNED>(ring.take(pr, k), at, r);
+                ring.read(pr, k, at, r);
                 add8(h[k], r);
             }
             // (blocks of an ALIGNED row are whole or hold the zeros they were cleared to)
             if constexpr (!ALIGNED) mask_from(h[k], c + 256 * k, cols, 0.f);
         }
-        if (STAGES == 1) fetch_row(row + step, at + step_at);
         if (a.h) {
+            if constexpr (ALIGNED) {
 #pragma unroll
-            for (int k = 0; k < NV; k++) store_block<TYPE, ALIGNED>(a.h, at, c + 256 * k, cols, h[k]);
+                for (int k = 0; k < NV; k++) store_block<TYPE, true>(a.h, at, c + 256 * k, cols, h[k]);
+            } else {
+                ring.store(a.h, at, c, cols, h, px);
+            }
         }
         float2 s = make_float2(0.f, 0.f);
 #pragma unroll
@@ -157,8 +161,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? 2 : 1) norm_fo
                     fma2(h[k][e + 2], h[k][e + 3], h[k][e + 2], h[k][e + 3], w.z, w.w, b.z, b.w);
                 }
             }
-            store_block<TYPE, ALIGNED>(a.y, at, c + 256 * k, cols, h[k]);
+            if constexpr (ALIGNED) store_block<TYPE, true>(a.y, at, c + 256 * k, cols, h[k]);
         }
+        if constexpr (!ALIGNED) ring.store(a.y, at, c, cols, h, px);
+        if (STAGES == 1) fetch_row(row + step, at + step_at);
     }
 }
 
@@ -186,8 +192,7 @@ template <u32 TYPE> static void launch_type(const NormArgs &a, cudaStream_t st)
 int launch_norm(NormArgs &a, u32 type, cudaStream_t st)
 {
     if (a.rows == 0) return ADACOMP_OK;
-    // (four blocks of unaligned binary32 rows, which take three chunks each, would not fit into shared memory)
-    norm_split(a, a.cols % 8u == 0 || type != ADACOMP_TYPE_F32 ? 4u : 2u);
+    norm_split(a, 4u);
     if (type == ADACOMP_TYPE_F32) launch_type<ADACOMP_TYPE_F32>(a, st);
     else if (type == ADACOMP_TYPE_BF16) launch_type<ADACOMP_TYPE_BF16>(a, st);
     else launch_type<ADACOMP_TYPE_F16>(a, st);

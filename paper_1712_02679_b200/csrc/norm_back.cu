@@ -23,13 +23,14 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? 2 : 1) norm_ba
     u64 row = (u64)set * a.groups + rg.g, at = row * a.cols + c0;
     const bool more = a.dh_in != nullptr;
     constexpr int STAGES = norm_stages(NV, THREADS);
-    const Ring<TYPE, ALIGNED, NV, THREADS, STAGES> ring = {dynamic + threadIdx.x, more ? 3u : 2u};
+    const Ring<TYPE, ALIGNED, NV, THREADS, STAGES> ring(dynamic, more ? 3u : 2u);
     float4 *params = reinterpret_cast<float4 *>(ring.end());
     float next_mean = 0.f, next_rstd = 0.f;
     u32 turn = 0;
     auto fetch_row = [&](u64 r, u64 r_at) {
         const u32 end = r < a.rows ? cols : 0u;
         if (r < a.rows) next_mean = a.mean[r], next_rstd = a.rstd[r];
+        ring.release();
         ring.copy(ring.place(turn, 0), a.dy, r_at, c, end);
         ring.copy(ring.place(turn, 1), a.x, r_at, c, end);
         if (more) ring.copy(ring.place(turn, 2), a.dh_in, r_at, c, end);
@@ -66,13 +67,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? 2 : 1) norm_ba
         turn ^= 1u;
         if (STAGES == 2) fetch_row(row + step, at + step_at);   // the next row is on its way while this one is worked on
         ring.wait();
-        const uint4 *py = ring.place(turn ^ 1u, 0), *ph = ring.place(turn ^ 1u, 1), *pi = ring.place(turn ^ 1u, 2);
+        uint4 *py = ring.place(turn ^ 1u, 0), *ph = ring.place(turn ^ 1u, 1), *pi = ring.place(turn ^ 1u, 2);
         float g[NV][8], xh[NV][8];
         float2 s1 = make_float2(0.f, 0.f), s2 = make_float2(0.f, 0.f);
 #pragma unroll
         for (int k = 0; k < NV; k++) {
-            unpack<TYPE, ALIGNED>(ring.take(py, k), at, g[k]);
-            unpack<TYPE, ALIGNED>(ring.take(ph, k), at, xh[k]);
+            ring.read(py, k, at, g[k]);
+            ring.read(ph, k, at, xh[k]);
             if constexpr (!ALIGNED) {           // (blocks of an ALIGNED row are whole or hold zeros)
                 mask_from(g[k], c + 256 * k, cols, 0.f);
                 mask_from(xh[k], c + 256 * k, cols, 0.f);
@@ -117,20 +118,23 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? 2 : 1) norm_ba
             for (int e = 0; e < 8; e += 2) fma2(g[k][e], g[k][e + 1], xh[k][e], xh[k][e + 1], m2, m2, g[k][e], g[k][e + 1]);
             if (more) {
                 float in[8];
-                unpack<TYPE, ALIGNED>(ring.take(pi, k), at, in);
+                ring.read(pi, k, at, in);
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) fma2(g[k][e], g[k][e + 1], g[k][e], g[k][e + 1], rstd, rstd, in[e], in[e + 1]);
             } else {
                 mul8(g[k], rstd);
             }
-            if (a.dresidual) store_block<TYPE, ALIGNED>(a.dresidual, at, c + 256 * k, cols, g[k]);
-            if constexpr (DROP) {
+        }
+        if (a.dresidual) ring.store(a.dresidual, at, c, cols, g, py);
+        if constexpr (DROP) {
+#pragma unroll
+            for (int k = 0; k < NV; k++) {
                 u32 bits[4];
                 drop_words(d, (u32)row, (c0 + c + 256 * k) >> 3, bits);
                 drop_apply(d, bits, g[k]);
             }
-            if (a.dx) store_block<TYPE, ALIGNED>(a.dx, at, c + 256 * k, cols, g[k]);
         }
+        if (a.dx) ring.store(a.dx, at, c, cols, g, py);
         if (STAGES == 1) fetch_row(row + step, at + step_at);
     }
     after_kernel_may_start();

@@ -14,12 +14,6 @@
 #ifndef MBU
 #define MBU 2u
 #endif
-#ifndef RUNF
-#define RUNF 16u
-#endif
-#ifndef RUNB
-#define RUNB 16u
-#endif
 namespace adacomp_impl {
 
 // How rows are shared, by the sizes alone.  A warp per row with up to `most` blocks of eight per lane; longer rows take up
@@ -50,13 +44,18 @@ void softmax_split(SoftmaxArgs &a, bool back, bool aligned)
     a.threads = a.tpr <= (u32)kSoftShort ? kSoftShort : kSoftThreads;
     a.groups = a.cluster == 1 && a.tpr < kSoftShort ? kSoftShort / a.tpr : 1u;
     while (a.groups > 1 && a.groups > a.q_len) a.groups /= 2;
-    // runs long enough to lay out the head's bias rarely, short enough for four CTAs' worth of work per place on the GPU
-    const u64 places = (u64)kBlockSms * 16 * 32 / a.tpr;
-    u64 run = rows / (places * 4);
-    const u32 longest = back ? RUNB : RUNF;
-    run = run < 1 ? 1 : run > longest ? longest : run;
-    const u32 top = (a.q_len + a.groups - 1) / a.groups;
-    a.run = run < top ? (u32)run : top ? top : 1u;
+    // Rows that a group takes one after the other: a CTA lays out the head's bias (and adds up its gradient) once for them,
+    // which costs it about `fixed` rows' work; against that stands the end of the launch, where about one CTA's work is
+    // spent on an emptying GPU.
+    const u64 fixed = back ? 4 : 2, heads = (u64)a.batch * a.heads;
+    const u64 slots = (u64)kBlockSms * (back ? 12 : 16) * 32 / (a.tpr * a.groups);
+    u64 best = ~0ull;
+    a.run = 1;
+    for (u32 run = 1; run <= 32u; run++) {
+        const u64 ctas = heads * ((a.q_len + a.groups * run - 1) / (a.groups * run)) * a.cluster;
+        const u64 cost = (ctas + slots) * (run + fixed);
+        if (cost < best) best = cost, a.run = run;
+    }
     a.chunks = (a.q_len + a.groups * a.run - 1) / (a.groups * a.run);
 }
 
@@ -66,22 +65,23 @@ template <u32 TYPE, bool ALIGNED, int NV, bool DROP, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SFB : 1) softmax_forward(const SoftmaxArgs a)
 {
     extern __shared__ uint4 dynamic[];
+    __shared__ unsigned short first[ADACOMP_MAX_BUCKETS];
     __shared__ float2 part[2][THREADS / 32];
     __shared__ float2 peers[2][8];
     const RowGroup rg(a.tpr);
     const SoftmaxRows rows(a, rg);
     const u32 c = block_column<NV>(0, rg.t);                // block k starts at c + 256 k
-    const Ring<TYPE, ALIGNED, NV, THREADS, 2> ring = {dynamic + threadIdx.x, 1u};
+    const Ring<TYPE, ALIGNED, NV, THREADS, 2> ring(dynamic, 1u);
     float *bias = reinterpret_cast<float *>(ring.end());
     u32 turn = 0;
     auto fetch_row = [&](u32 i) {
         const u64 at = ((u64)rows.bh * a.q_len + i) * a.ld + rows.c0;
+        ring.release();
         ring.copy(ring.place(turn, 0), a.scores, at, c, i < rows.i1 ? rows.end(a, i) : 0u);
         copies_commit();
     };
     fetch_row(rows.i0);
-    build_bias(a, rows.bh % a.heads, bias);
-    __syncthreads();
+    build_bias(a, rows.bh % a.heads, bias, first);
     if (a.cluster > 1) cg::this_cluster().sync();      // every CTA of the cluster runs before its memory is written
     Drop d;
     if constexpr (DROP) d = drop_begin(a.drop);
@@ -94,55 +94,51 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SFB : 1) soft
         turn ^= 1u;
         fetch_row(i + 1);               // the next row is on its way while this one is worked on
         ring.wait();
-        const uint4 *place = ring.place(turn ^ 1u, 0);
+        uint4 *place = ring.place(turn ^ 1u, 0);
         const int live = rows.live<NV>(end, c - 8 * rg.lane);
-        float v[NV][8];
-        float top, about, s;
         with_blocks<NV>(live, [&](auto blocks) {
             constexpr int L = decltype(blocks)::value;
+            float v[NV][8];
             float t0 = -INFINITY, t1 = -INFINITY;
 #pragma unroll
             for (int k = 0; k < L; k++) {
-                unpack<TYPE, ALIGNED>(ring.take(place, k), at, v[k]);
+                ring.read(place, k, at, v[k]);
                 add_bias(v[k], bias, (int)a.reach, a.scale, d0 + (int)(c + 256 * k));
-                mask_from(v[k], c + 256 * k, end, -INFINITY);
+                if (k == L - 1) mask_from(v[k], c + 256 * k, end, -INFINITY);     // (those before it are whole)
 #pragma unroll
                 for (int e = 0; e < 8; e += 4) {
                     t0 = fmaxf(fmaxf(t0, v[k][e]), v[k][e + 1]);
                     t1 = fmaxf(fmaxf(t1, v[k][e + 2]), v[k][e + 3]);
                 }
             }
-            top = warp_max(fmaxf(t0, t1));
-            about = top == -INFINITY ? 0.f : top;
+            float top = warp_max(fmaxf(t0, t1));
+            const float about = top == -INFINITY ? 0.f : top;
             exp_about<L>(v, about);
             float2 sums = make_float2(0.f, 0.f);
 #pragma unroll
             for (int k = 0; k < L; k++) sum8(sums, v[k]);
-            s = warp_sum(sums.x + sums.y);
-        });
-        if (rg.warps > 1) {
-            if (rg.lane == 0) part[parity][rg.first_warp + rg.warp] = make_float2(top, s);
-            rg.sync();
-            const u32 w = rg.lane & 15u;
-            const float2 p = w < rg.warps ? part[parity][rg.first_warp + w] : make_float2(-INFINITY, 0.f);
-            top = warp_max(p.x);
-            s = half_sum(p.y * exp2_fast((p.x - (top == -INFINITY ? 0.f : top)) * kLog2e));
-        }
-        if (a.cluster > 1) {
-            cg::cluster_group cl = cg::this_cluster();
-            if (threadIdx.x < a.cluster) cl.map_shared_rank(&peers[parity][0], threadIdx.x)[rows.rank] = make_float2(top, s);
-            cl.sync();
-            for (u32 j = 0; j < a.cluster; j++) top = fmaxf(top, peers[parity][j].x);
-            s = 0.f;
-            for (u32 j = 0; j < a.cluster; j++)
-                s += peers[parity][j].y * exp2_fast((peers[parity][j].x - (top == -INFINITY ? 0.f : top)) * kLog2e);
-        }
-        // a row that keeps nothing has s = 0 and becomes zeros
-        float f = s == 0.f ? 0.f : exp2_fast((about - (top == -INFINITY ? 0.f : top)) * kLog2e) * __fdividef(1.f, s);
-        if (a.lse && rg.t == 0 && rows.rank == 0) a.lse[row] = s == 0.f ? -INFINITY : fmaf(__log2f(s), kLn2, top);
-        if constexpr (DROP) f *= d.factor;
-        with_blocks<NV>(live, [&](auto blocks) {
-            constexpr int L = decltype(blocks)::value;
+            float s = warp_sum(sums.x + sums.y);
+            if (rg.warps > 1) {
+                if (rg.lane == 0) part[parity][rg.first_warp + rg.warp] = make_float2(top, s);
+                rg.sync();
+                const u32 w = rg.lane & 15u;
+                const float2 p = w < rg.warps ? part[parity][rg.first_warp + w] : make_float2(-INFINITY, 0.f);
+                top = warp_max(p.x);
+                s = half_sum(p.y * exp2_fast((p.x - (top == -INFINITY ? 0.f : top)) * kLog2e));
+            }
+            if (a.cluster > 1) {
+                cg::cluster_group cl = cg::this_cluster();
+                if (threadIdx.x < a.cluster) cl.map_shared_rank(&peers[parity][0], threadIdx.x)[rows.rank] = make_float2(top, s);
+                cl.sync();
+                for (u32 j = 0; j < a.cluster; j++) top = fmaxf(top, peers[parity][j].x);
+                s = 0.f;
+                for (u32 j = 0; j < a.cluster; j++)
+                    s += peers[parity][j].y * exp2_fast((peers[parity][j].x - (top == -INFINITY ? 0.f : top)) * kLog2e);
+            }
+            // a row that keeps nothing has s = 0 and becomes zeros
+            float f = s == 0.f ? 0.f : exp2_fast((about - (top == -INFINITY ? 0.f : top)) * kLog2e) * __fdividef(1.f, s);
+            if (a.lse && rg.t == 0 && rows.rank == 0) a.lse[row] = s == 0.f ? -INFINITY : fmaf(__log2f(s), kLn2, top);
+            if constexpr (DROP) f *= d.factor;
 #pragma unroll
             for (int k = 0; k < L; k++) mul8(v[k], f);
             if constexpr (DROP) drop_row<L>(d, (u32)row, (rows.c0 + c) >> 3, v);
@@ -150,8 +146,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SFB : 1) soft
             for (int k = L; k < NV; k++)
 #pragma unroll
                 for (int e = 0; e < 8; e++) v[k][e] = 0.f;
-#pragma unroll
-            for (int k = 0; k < NV; k++) store_block<TYPE, ALIGNED>(a.probs, at, c + 256 * k, rows.cols, v[k]);
+            ring.store(a.probs, at, c, rows.cols, v, place);
         });
     }
 }

@@ -49,25 +49,35 @@ template <int L, int NV> __device__ inline void exp_about(float (&v)[NV][8], flo
 __host__ __device__ inline u32 bias_entries(u32 reach) { return (2 * reach + 16 + 1 + 3) & ~3u; }
 __host__ __device__ inline u32 bias_floats(u32 reach) { return 4 * bias_entries(reach); }
 
-__device__ inline u32 bucket_of(const SoftmaxArgs &a, int d)
+// The first distances of the buckets, in shared memory for the search.
+__device__ inline void load_first(const SoftmaxArgs &a, unsigned short *first)
+{
+    for (u32 i = threadIdx.x; i < a.side; i += blockDim.x) first[i] = a.first[i];
+}
+
+__device__ inline u32 bucket_of(const SoftmaxArgs &a, const unsigned short *first, int d)
 {
     const u32 away = d <= 0 ? (u32)-d : a.both ? (u32)d : 0u;
-    u32 b = 0;
-    for (u32 k = 1; k < a.side; k++) b += a.first[k] <= away ? 1u : 0u;
+    u32 b = 0;                  // the last one whose first distance is not beyond `away`
+    for (u32 step = a.search; step > 0; step >>= 1)
+        if (b + step < a.side && first[b + step] <= away) b += step;
     return d > 0 && a.both ? b + a.side : b;
 }
 
-// Called by all threads of the CTA; the caller synchronises.
-__device__ inline void build_bias(const SoftmaxArgs &a, u32 head, float *bias)
+// Called by all threads of the CTA, which meet twice.
+__device__ inline void build_bias(const SoftmaxArgs &a, u32 head, float *bias, unsigned short *first)
 {
+    load_first(a, first);
+    __syncthreads();
     const int reach = (int)a.reach, n = (int)bias_entries(a.reach);
     for (int i = (int)threadIdx.x; i < n + 3; i += (int)blockDim.x) {
         const int d = max(-reach, min(reach, i - 8 - reach));
-        const float v = a.table ? a.table[(u64)bucket_of(a, d) * a.heads + head] : 0.f;
+        const float v = a.table ? a.table[bucket_of(a, first, d) * (size_t)a.heads + head] : 0.f;
 #pragma unroll
         for (int s = 0; s < 4; s++)
             if (i >= s && i - s < n) bias[s * n + i - s] = v;
     }
+    __syncthreads();
 }
 
 // v: scores of a block whose first distance is d, replaced by logits.

@@ -23,6 +23,7 @@ template <u32 TYPE, bool ALIGNED, int NV, bool DROP, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SBB : 1) softmax_backward(const SoftmaxArgs a)
 {
     extern __shared__ uint4 dynamic[];
+    __shared__ unsigned short first[ADACOMP_MAX_BUCKETS];
     __shared__ float part[2][THREADS / 32];
     __shared__ float2 ends[THREADS / 32];
     __shared__ float peers[2][8];
@@ -32,7 +33,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SBB : 1) soft
     const int reach = (int)a.reach;
     const u32 line = 2 * a.reach + 1, cta_warp = threadIdx.x >> 5, cta_warps = blockDim.x >> 5;
     constexpr int STAGES = soft_back_stages(NV, THREADS);
-    const Ring<TYPE, ALIGNED, NV, THREADS, STAGES> ring = {dynamic + threadIdx.x, 2u};
+    const Ring<TYPE, ALIGNED, NV, THREADS, STAGES> ring(dynamic, 2u);
     float *bias = reinterpret_cast<float *>(ring.end()), *all_sums = bias + bias_floats(a.reach);
     if (a.reach > kLineReach) all_sums = a.partial + (u64)gridDim.x * a.buckets + (u64)blockIdx.x * cta_warps * line;
     float *sums = all_sums + cta_warp * line;          // entry d + reach; those of -reach and reach stay 0
@@ -42,15 +43,15 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SBB : 1) soft
         const u64 row = (u64)rows.bh * a.q_len + i, at = row * a.ld + rows.c0;
         const u32 end = i < rows.i1 ? rows.end(a, i) : 0u;
         if (i < rows.i1) next_lse = a.lse[row];
+        ring.release();
         ring.copy(ring.place(turn, 0), a.scores, at, c, end);
         ring.copy(ring.place(turn, 1), a.dprobs, at, c, end);
         copies_commit();
     };
     fetch_row(rows.i0);
-    build_bias(a, rows.bh % a.heads, bias);
     if (a.partial)
         for (u32 i = rg.lane; i < line; i += 32) sums[i] = 0.f;
-    __syncthreads();
+    build_bias(a, rows.bh % a.heads, bias, first);
     if (a.cluster > 1) cg::this_cluster().sync();      // every CTA of the cluster runs before its memory is written
     Drop d;
     if constexpr (DROP) d = drop_begin(a.drop);
@@ -95,64 +96,52 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SBB : 1) soft
         if (STAGES == 2) fetch_row(i + 1);      // the next row is on its way while this one is worked on
         ring.wait();
         const int live = rows.live<NV>(end, c - 8 * rg.lane);
-        const uint4 *ps = ring.place(turn ^ 1u, 0), *pd = ring.place(turn ^ 1u, 1);
-        float p[NV][8], g[NV][8];
-        float dot;
+        uint4 *ps = ring.place(turn ^ 1u, 0), *pd = ring.place(turn ^ 1u, 1);
         with_blocks<NV>(live, [&](auto blocks) {
             constexpr int L = decltype(blocks)::value;
+            float p[NV][8], g[L][8];
 #pragma unroll
             for (int k = 0; k < L; k++) {
-                unpack<TYPE, ALIGNED>(ring.take(ps, k), at, p[k]);
-                unpack<TYPE, ALIGNED>(ring.take(pd, k), at, g[k]);
+                ring.read(ps, k, at, p[k]);
+                ring.read(pd, k, at, g[k]);
                 add_bias(p[k], bias, reach, a.scale, (int)(rows.c0 + c + 256 * k) - pos);
-                mask_from(p[k], c + 256 * k, end, -INFINITY);
-                mask_from(g[k], c + 256 * k, end, 0.f);
+                if (k == L - 1) {               // (those before it are whole)
+                    mask_from(p[k], c + 256 * k, end, -INFINITY);
+                    mask_from(g[k], c + 256 * k, end, 0.f);
+                }
             }
             if constexpr (DROP) drop_row<L>(d, (u32)row, (rows.c0 + c) >> 3, g);      // (the factor comes where dp is used)
             exp_about<L>(p, lse == -INFINITY ? 0.f : lse);
             float2 dots = make_float2(0.f, 0.f);
 #pragma unroll
             for (int k = 0; k < L; k++) dot8(dots, p[k], g[k]);
-            dot = dots.x + dots.y;
+            float dot = dots.x + dots.y;
+            // A sum's logarithm does not show beside a statistic this large (ulp 2^-9 and up): P is then normalised again.
+            // (A property of the row, so that all its threads meet in row_sum.)
+            if (lse != -INFINITY && fabsf(lse) > 16384.f) {
+                float2 total = make_float2(0.f, 0.f);
 #pragma unroll
-            for (int k = L; k < NV; k++)
+                for (int k = 0; k < L; k++) sum8(total, p[k]);
+                const float sum = row_sum(total.x + total.y), f = sum == 0.f ? 0.f : 1.f / sum;
+                dot *= f;
 #pragma unroll
-                for (int e = 0; e < 8; e++) p[k][e] = 0.f;
-        });
-        if (STAGES == 1) fetch_row(i + 1);
-        // A sum's logarithm does not show beside a statistic this large (ulp 2^-9 and up): P is then normalised again.
-        // (A property of the row, so that all its threads meet in row_sum.)
-        if (lse != -INFINITY && fabsf(lse) > 16384.f) {
-            float total = 0.f;
-#pragma unroll
-            for (int k = 0; k < NV; k++)
-#pragma unroll
-                for (int e = 0; e < 8; e++) total += p[k][e];
-            total = row_sum(total);
-            const float f = total == 0.f ? 0.f : 1.f / total;
-            dot *= f;
-#pragma unroll
-            for (int k = 0; k < NV; k++)
-#pragma unroll
-                for (int e = 0; e < 8; e++) p[k][e] *= f;
-        }
-        const float factor = DROP ? d.factor : 1.f;
-        dot = row_sum(dot) * factor;
-        float carry = 0.f;              // lane 0: the last sum of the block before
-        with_blocks<NV>(live, [&](auto blocks) {
-            constexpr int L = decltype(blocks)::value;
-#pragma unroll
-            for (int k = 0; k < L; k++) {
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    if (DROP) fma2(g[k][e], g[k][e + 1], g[k][e], g[k][e + 1], factor, factor, -dot, -dot);
-                    else add2(g[k][e], g[k][e + 1], g[k][e], g[k][e + 1], -dot, -dot);
-                }
-                mul8(p[k], g[k]);
+                for (int k = 0; k < L; k++) mul8(p[k], f);
             }
-            if (a.partial) {
+            const float factor = DROP ? d.factor : 1.f;
+            dot = row_sum(dot) * factor;
+            float carry = 0.f;              // lane 0: the last sum of the block before
 #pragma unroll
-                for (int k = 0; k < NV; k++) {
+            for (int k = 0; k < NV; k++) {
+                if (k < L) {
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        float(&x)[8] = g[k < L ? k : 0];
+                        if (DROP) fma2(x[e], x[e + 1], x[e], x[e + 1], factor, factor, -dot, -dot);
+                        else add2(x[e], x[e + 1], x[e], x[e + 1], -dot, -dot);
+                    }
+                    mul8(p[k], g[k < L ? k : 0]);
+                }
+                if (a.partial) {
                     const float from = __shfl_sync(kAllLanes, acc[k][7], (rg.lane + 31u) & 31u);
 #pragma unroll
                     for (int e = 7; e > 0; e--) acc[k][e] = k < L ? acc[k][e - 1] + p[k][e] : acc[k][e - 1];
@@ -160,23 +149,40 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SBB : 1) soft
                     if (k < L) acc[k][0] += p[k][0];
                     carry = from;
                 }
-            }
+                if (k < L) {
+                    mul8(p[k], a.scale);
+                } else {
 #pragma unroll
-            for (int k = 0; k < NV; k++) {
-                if (k < L) mul8(p[k], a.scale);
-                store_block<TYPE, ALIGNED>(a.dscores, at, c + 256 * k, rows.cols, p[k]);
+                    for (int e = 0; e < 8; e++) p[k][e] = 0.f;
+                }
             }
+            ring.store(a.dscores, at, c, rows.cols, p, ps);
+            if (STAGES == 1) fetch_row(i + 1);
+            if (a.partial && rg.lane == 0 && i > rows.i0) put(last_col - (pos - 1), carry);
         });
-        if (a.partial && rg.lane == 0 && i > rows.i0) put(last_col - (pos - 1), carry);
     }
     if (!a.partial) return;
     __syncwarp();
     if (rows.i1 > rows.i0) {
         const int pos = (int)(rows.i1 - 1u) + a.q_offset;
 #pragma unroll
-        for (int k = 0; k < NV; k++)
+        for (int k = 0; k < NV; k++) {
+            const int d0 = (int)(rows.c0 + c + 256 * k) - pos, warp0 = d0 - 8 * (int)rg.lane;     // the warp's first distance
+            if (warp0 >= reach || warp0 + 255 <= -reach) {
+                float2 far = make_float2(0.f, 0.f);
+                sum8(far, acc[k]);
+                if (warp0 >= reach) behind += far.x + far.y;
+                else before += far.x + far.y;
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; e++) put((int)(rows.c0 + c + 256 * k) + e - pos, acc[k][e]);
+                for (int e = 0; e < 8; e++) {
+                    const int d = d0 + e;
+                    if (d >= reach) behind += acc[k][e];
+                    if (d <= -reach) before += acc[k][e];
+                    if (d < reach && d > -reach) sums[d + reach] += acc[k][e];
+                }
+            }
+        }
     }
     after_kernel_may_start();
     before = warp_sum(before);
