@@ -587,7 +587,7 @@ typedef struct adacomp_relpos {
 int adacomp_relpos_plan(uint32_t num_buckets, uint32_t max_distance, uint32_t bidirectional, adacomp_relpos *plan);
 
 typedef struct adacomp_softmax_options {
-    uint32_t batch, heads, q_len, k_len;    /* k_len <= ADACOMP_MAX_KEYS */
+    uint32_t batch, heads, q_len, k_len;    /* batch * heads * q_len < 2^31, k_len <= ADACOMP_MAX_KEYS */
     uint64_t ld;            /* elements from one row to the next, >= k_len; rows are otherwise dense */
     uint32_t type;
     float scale;

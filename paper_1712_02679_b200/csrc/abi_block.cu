@@ -1,5 +1,6 @@
 // C ABI of the operators of a transformer block (include/adacomp.h): argument checks, then the launchers in dropout.cu,
 // norm*.cu and softmax*.cu.
+#include <float.h>
 #include <math.h>
 #include <initializer_list>
 
@@ -56,7 +57,7 @@ static int check_softmax(const float *table, const adacomp_relpos *relpos, const
     if (opt->type > ADACOMP_TYPE_F16) return ADACOMP_ERR_TYPE;
     const u64 heads = (u64)opt->batch * opt->heads;
     if (opt->k_len > ADACOMP_MAX_KEYS || opt->ld < opt->k_len || opt->q_len >= (1u << 30) || opt->q_offset > (1 << 30) ||
-        opt->q_offset < -(1 << 30) || heads >= (1ull << 32) || (opt->q_len && heads >= (1ull << 32) / opt->q_len))
+        opt->q_offset < -(1 << 30) || heads >= (1ull << 31) || (opt->q_len && heads >= (1ull << 31) / opt->q_len))
         return ADACOMP_ERR_SHAPE;
     if (!isfinite(opt->scale)) return ADACOMP_ERR_VALUE;
     a.batch = opt->batch;
@@ -64,7 +65,8 @@ static int check_softmax(const float *table, const adacomp_relpos *relpos, const
     a.q_len = opt->q_len;
     a.k_len = opt->k_len;
     a.ld = opt->ld;
-    a.scale = opt->scale;
+    a.out_scale = opt->scale;
+    a.scale = opt->scale != 0.f ? opt->scale : FLT_TRUE_MIN;
     a.causal = opt->causal;
     a.q_offset = opt->q_offset;
     a.key_len = opt->key_len;

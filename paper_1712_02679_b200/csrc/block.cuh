@@ -102,11 +102,6 @@ template <u32 TYPE> __device__ inline void store1(void *base, u64 e, float v)
 // issues, not by how many operations it has units for
 // ---------------------------------------------------------------------------------
 
-#ifdef SCALAR
-__device__ inline void fma2(float &d0, float &d1, float a0, float a1, float b0, float b1, float c0, float c1) { d0 = fmaf(a0,b0,c0); d1 = fmaf(a1,b1,c1); }
-__device__ inline void mul2(float &d0, float &d1, float a0, float a1, float b0, float b1) { d0 = a0*b0; d1 = a1*b1; }
-__device__ inline void add2(float &d0, float &d1, float a0, float a1, float b0, float b1) { d0 = a0+b0; d1=a1+b1; }
-#else
 __device__ inline void fma2(float &d0, float &d1, float a0, float a1, float b0, float b1, float c0, float c1)
 {
     asm("{\n\t.reg .b64 a, b, c, d;\n\t"
@@ -132,7 +127,6 @@ __device__ inline void add2(float &d0, float &d1, float a0, float a1, float b0, 
         : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
 }
 
-#endif
 // v = v * x + y, v * x, v + x, element by element or with one number
 __device__ inline void fma8(float (&v)[8], float x, float y)
 {
@@ -427,16 +421,45 @@ template <u32 TYPE, bool ALIGNED, int NV, int THREADS, int STAGES> struct Ring {
         }
         widen8<TYPE>(r, v);
     }
+    // The row's elements from column `last` on, in blocks `first` to `count` - 1, become `bits` (an element, repeated).
+    __device__ static void fill(uint4 *row, u64 row_at, u32 c, u32 last, int first, int count, u32 bits)
+    {
+        const int s = ALIGNED ? 0 : (int)((u32)row_at & (kPer - 1u));
+        if (!ALIGNED) __syncwarp();
+        // (not ALIGNED: one chunk more, which only the last lane's last block has to itself)
+#pragma unroll 1
+        for (int k = first; k < count; k++)
+#pragma unroll
+            for (int i = 0; i < kChunks + (ALIGNED ? 0 : 1); i++) {
+                if (i == kChunks && threadIdx.x % 32u != 31u) continue;
+                const int keep = (int)last - ((int)(c + 256 * k + i * kPer) - s);       // elements of this chunk that stay
+                uint4 *p = row + at(k, i);
+                if (keep <= 0) {
+                    *p = make_uint4(bits, bits, bits, bits);
+                } else if (keep < (int)kPer) {
+                    uint4 q = *p;
+                    u32 *w = reinterpret_cast<u32 *>(&q);
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        if (TYPE == ADACOMP_TYPE_F32) w[j] = j < keep ? w[j] : bits;
+                        else w[j] = 2 * j + 1 < keep ? w[j] : 2 * j < keep ? __byte_perm(w[j], bits, 0x5410) : bits;
+                    }
+                    *p = q;
+                }
+            }
+        if (!ALIGNED) __syncwarp();
+    }
     // Places that no copy reaches, where the kernel counts on zeros behind a row's end.
     __device__ void clear(u32 c, u32 last) const
     {
-        if (!ALIGNED) return;
-        for (u32 j = 0; j < STAGES * arrays; j++)
+        if constexpr (ALIGNED) {
+            for (u32 j = 0; j < STAGES * arrays; j++)
 #pragma unroll
-            for (int k = 0; k < NV; k++)
+                for (int k = 0; k < NV; k++)
 #pragma unroll
-                for (int i = 0; i < kChunks; i++)
-                    if (c + 256 * k >= last) mine[j * kArray + at(k, i)] = make_uint4(0u, 0u, 0u, 0u);
+                    for (int i = 0; i < kChunks; i++)
+                        if (c + 256 * k >= last) mine[j * kArray + at(k, i)] = make_uint4(0u, 0u, 0u, 0u);
+        }
     }
     // Stores the row's columns before `cols`; `line`: places of this thread's row that have been read, which a row that is
     // not ALIGNED goes through.

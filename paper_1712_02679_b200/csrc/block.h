@@ -69,7 +69,7 @@ struct SoftmaxArgs {
     int q_offset;
     // softmax_split: as above; rows a group of threads takes one after the other, and a CTA's chunks per head
     u32 tpr, per, threads, groups, cluster, slice, run, chunks;
-    float scale;
+    float scale, out_scale;                      // scale: 0 is replaced by the smallest number, so that -inf masks stay
     DropArgs drop;
     u32 buckets, side, both, reach;              // the bias: see include/adacomp.h (adacomp_relpos)
     u32 search;                                  // the largest power of two below `side` (0: none)
@@ -79,7 +79,7 @@ struct SoftmaxArgs {
 // softmax.cu, softmax_back.cu
 int launch_softmax(SoftmaxArgs &a, u32 type, cudaStream_t st);
 int launch_softmax_back(SoftmaxArgs &a, u32 type, cudaStream_t st);
-void softmax_split(SoftmaxArgs &a, bool back, bool aligned);
+void softmax_split(SoftmaxArgs &a, bool back);
 size_t softmax_workspace(SoftmaxArgs &a);
 
 }  // namespace adacomp_impl

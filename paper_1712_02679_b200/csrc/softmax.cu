@@ -2,29 +2,17 @@
 // scale, the causal and length masks and dropout, in one pass.
 #include "softmax.cuh"
 
-#ifndef SFB
-#define SFB 4
-#endif
-#ifndef MF
-#define MF 4u
-#endif
-#ifndef MB
-#define MB 4u
-#endif
-#ifndef MBU
-#define MBU 2u
-#endif
 namespace adacomp_impl {
 
-// How rows are shared, by the sizes alone.  A warp per row with up to `most` blocks of eight per lane; longer rows take up
+// How rows are shared, by the sizes alone.  A warp per row with up to four blocks of eight per lane; longer rows take up
 // to 16 warps, then a cluster of up to 8 CTAs.  The backward pass holds three numbers per element and takes half the blocks
 // per lane where a CTA has all 16 warps.  Few long rows are cut up further, until every SM has a CTA.
-void softmax_split(SoftmaxArgs &a, bool back, bool aligned)
+void softmax_split(SoftmaxArgs &a, bool back)
 {
-    const u32 blocks = (a.k_len + 7u) / 8u, most = !back ? MF : aligned ? MB : MBU;
+    const u32 blocks = (a.k_len + 7u) / 8u;
     const u64 rows = (u64)a.batch * a.heads * a.q_len;
     a.cluster = 1;
-    a.per = blocks <= 32u ? 1u : blocks <= 64u || most == 2u ? 2u : 4u;
+    a.per = blocks <= 32u ? 1u : blocks <= 64u ? 2u : 4u;
     if (blocks <= 32u * a.per) {
         a.tpr = 32;
     } else {
@@ -51,7 +39,8 @@ void softmax_split(SoftmaxArgs &a, bool back, bool aligned)
     const u64 slots = (u64)kBlockSms * (back ? 12 : 16) * 32 / (a.tpr * a.groups);
     u64 best = ~0ull;
     a.run = 1;
-    for (u32 run = 1; run <= 32u; run++) {
+    const u32 longest = (a.q_len + a.groups - 1) / a.groups;
+    for (u32 run = 1; run <= 32u && run <= longest; run++) {
         const u64 ctas = heads * ((a.q_len + a.groups * run - 1) / (a.groups * run)) * a.cluster;
         const u64 cost = (ctas + slots) * (run + fixed);
         if (cost < best) best = cost, a.run = run;
@@ -62,7 +51,7 @@ void softmax_split(SoftmaxArgs &a, bool back, bool aligned)
 // A row stays in registers.  Each warp takes powers of two about its own maximum; the maxima and sums of the row's warps
 // are joined in one meeting, and what a warp holds is rescaled as it is stored.
 template <u32 TYPE, bool ALIGNED, int NV, bool DROP, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SFB : 1) softmax_forward(const SoftmaxArgs a)
+__global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? 4 : 1) softmax_forward(const SoftmaxArgs a)
 {
     extern __shared__ uint4 dynamic[];
     __shared__ unsigned short first[ADACOMP_MAX_BUCKETS];
@@ -71,6 +60,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SFB : 1) soft
     const RowGroup rg(a.tpr);
     const SoftmaxRows rows(a, rg);
     const u32 c = block_column<NV>(0, rg.t);                // block k starts at c + 256 k
+    const u32 warp_c = block_column<NV>(0, rg.t & ~31u);    // and the warp's at warp_c + 256 k
     const Ring<TYPE, ALIGNED, NV, THREADS, 2> ring(dynamic, 1u);
     float *bias = reinterpret_cast<float *>(ring.end());
     u32 turn = 0;
@@ -85,6 +75,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SFB : 1) soft
     if (a.cluster > 1) cg::this_cluster().sync();      // every CTA of the cluster runs before its memory is written
     Drop d;
     if constexpr (DROP) d = drop_begin(a.drop);
+    const u32 masked = masked_score<TYPE>(a.scale);
     u32 parity = 0;
 #pragma unroll 1
     for (u32 i = rows.i0; i < rows.i1; i++, parity ^= 1u) {
@@ -95,16 +86,16 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SFB : 1) soft
         fetch_row(i + 1);               // the next row is on its way while this one is worked on
         ring.wait();
         uint4 *place = ring.place(turn ^ 1u, 0);
-        const int live = rows.live<NV>(end, c - 8 * rg.lane);
-        with_blocks<NV>(live, [&](auto blocks) {
+        const int live = rows.live<NV>(end, warp_c);
+        with_blocks<NV>(live, !a.causal, [&](auto blocks) {
             constexpr int L = decltype(blocks)::value;
+            if (end < warp_c + 256 * L) ring.fill(place, at, c, end, end > warp_c ? (int)((end - warp_c) / 256u) : 0, L, masked);
             float v[NV][8];
             float t0 = -INFINITY, t1 = -INFINITY;
 #pragma unroll
             for (int k = 0; k < L; k++) {
                 ring.read(place, k, at, v[k]);
                 add_bias(v[k], bias, (int)a.reach, a.scale, d0 + (int)(c + 256 * k));
-                if (k == L - 1) mask_from(v[k], c + 256 * k, end, -INFINITY);     // (those before it are whole)
 #pragma unroll
                 for (int e = 0; e < 8; e += 4) {
                     t0 = fmaxf(fmaxf(t0, v[k][e]), v[k][e + 1]);
@@ -179,7 +170,7 @@ template <u32 TYPE> static void launch_type(const SoftmaxArgs &a, cudaStream_t s
 int launch_softmax(SoftmaxArgs &a, u32 type, cudaStream_t st)
 {
     if ((u64)a.batch * a.heads * a.q_len == 0) return ADACOMP_OK;
-    softmax_split(a, false, a.ld % 8u == 0);
+    softmax_split(a, false);
     if (type == ADACOMP_TYPE_F32) launch_type<ADACOMP_TYPE_F32>(a, st);
     else if (type == ADACOMP_TYPE_BF16) launch_type<ADACOMP_TYPE_BF16>(a, st);
     else launch_type<ADACOMP_TYPE_F16>(a, st);

@@ -22,23 +22,16 @@ __device__ inline float exp2_fast(float x)
     return y;
 }
 
-// v = e^(v - about) in the first L blocks, about not -inf.  The product with log2(e) is taken of the difference where that of `about` would
-// overflow: rows of a type's lowest value (a mask added by the caller) keep their softmax.
+// v = e^(v - about) in the first L blocks, about not -inf.  The product with log2(e) is taken of the difference: that of a
+// type's lowest value (a mask added by the caller) would overflow, and rows of nothing else keep their softmax this way.
 template <int L, int NV> __device__ inline void exp_about(float (&v)[NV][8], float about)
 {
-    if (fabsf(about) < 1e38f) {
-        const float about2 = -about * kLog2e;
 #pragma unroll
-        for (int k = 0; k < L; k++) {
-            fma8(v[k], kLog2e, about2);
+    for (int k = 0; k < L; k++) {
+        add8(v[k], -about);
+        mul8(v[k], kLog2e);
 #pragma unroll
-            for (int e = 0; e < 8; e++) v[k][e] = exp2_fast(v[k][e]);
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < L; k++)
-#pragma unroll
-            for (int e = 0; e < 8; e++) v[k][e] = exp2_fast((v[k][e] - about) * kLog2e);
+        for (int e = 0; e < 8; e++) v[k][e] = exp2_fast(v[k][e]);
     }
 }
 
@@ -92,6 +85,13 @@ __device__ inline void add_bias(float (&v)[8], const float *bias, int reach, flo
     fma2(v[6], v[7], v[6], v[7], scale, scale, y.z, y.w);
 }
 
+// What masked scores are replaced by before the arithmetic: an infinity whose product with the scale is -inf.
+template <u32 TYPE> __device__ inline u32 masked_score(float scale)
+{
+    const u32 inf = TYPE == ADACOMP_TYPE_F32 ? 0x7f800000u : TYPE == ADACOMP_TYPE_BF16 ? 0x7f807f80u : 0x7c007c00u;
+    return scale > 0.f ? inf | (TYPE == ADACOMP_TYPE_F32 ? 0x80000000u : 0x80008000u) : inf;
+}
+
 // Elements of the first L blocks that dropout drops become 0; blocks go through the generator two by two.
 template <int L, int NV> __device__ inline void drop_row(const Drop &d, u32 row, u32 group0, float (&v)[NV][8])
 {
@@ -110,14 +110,18 @@ template <int L, int NV> __device__ inline void drop_row(const Drop &d, u32 row,
     }
 }
 
-// f(L) for L = live as a compile-time number (0 counts as 1): the blocks of a row are worked on together, and those that
-// hold nothing not at all.
+// f(L) with a compile-time number L of blocks that are worked on together, at least the `live` ones (what lies far behind
+// a short row's end is not worked on at all).  `fine`: just as many as are live; else all or half of them.  Causal rows take
+// the latter: their ends differ from row to row, and an SM whose warps are in all the bodies at once waits for its
+// instruction cache (8 x 16 x 1024 x 1024, bf16, forward: 124 us against 138; rows of one length per sequence, ragged: 137
+// against 126).
 template <int L> struct Blocks { static constexpr int value = L; };
-template <int NV, typename F> __device__ inline void with_blocks(int live, F f)
+template <int NV, typename F> __device__ inline void with_blocks(int live, bool fine, F f)
 {
-    if (NV > 3 && live > 3) f(Blocks<NV>());
-    else if (NV > 2 && live > 2) f(Blocks<(NV > 2 ? 3 : NV)>());
-    else if (NV > 1 && live > 1) f(Blocks<(NV > 1 ? 2 : NV)>());
+    constexpr int HALF = (NV + 1) / 2;
+    if (NV == 1 || live > (fine ? NV - 1 : HALF)) f(Blocks<NV>());
+    else if (NV == 4 && live == 3) f(Blocks<(NV == 4 ? 3 : 1)>());
+    else if (NV == 4 && (!fine || live == 2)) f(Blocks<HALF>());
     else f(Blocks<1>());
 }
 

@@ -1,9 +1,6 @@
 // The biased softmax's backward pass: the scores' gradient and the bias table's.
 #include "softmax.cuh"
 
-#ifndef SBB
-#define SBB 3
-#endif
 namespace adacomp_impl {
 
 // P is formed again from the scores and the row's logarithm of the sum, dp = dropout'(dprobs), D = sum_j P dp, and
@@ -20,7 +17,7 @@ namespace adacomp_impl {
 __host__ __device__ constexpr int soft_back_stages(int nv, int threads) { return nv == 4 && threads == kSoftThreads ? 1 : 2; }
 
 template <u32 TYPE, bool ALIGNED, int NV, bool DROP, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SBB : 1) softmax_backward(const SoftmaxArgs a)
+__global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? 3 : 1) softmax_backward(const SoftmaxArgs a)
 {
     extern __shared__ uint4 dynamic[];
     __shared__ unsigned short first[ADACOMP_MAX_BUCKETS];
@@ -30,6 +27,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SBB : 1) soft
     const RowGroup rg(a.tpr);
     const SoftmaxRows rows(a, rg);
     const u32 c = block_column<NV>(0, rg.t);                // block k starts at c + 256 k
+    const u32 warp_c = block_column<NV>(0, rg.t & ~31u);    // and the warp's at warp_c + 256 k
     const int reach = (int)a.reach;
     const u32 line = 2 * a.reach + 1, cta_warp = threadIdx.x >> 5, cta_warps = blockDim.x >> 5;
     constexpr int STAGES = soft_back_stages(NV, THREADS);
@@ -60,6 +58,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SBB : 1) soft
     for (int k = 0; k < NV; k++)
 #pragma unroll
         for (int e = 0; e < 8; e++) acc[k][e] = 0.f;
+    const u32 masked = masked_score<TYPE>(a.scale);
     float before = 0.f, behind = 0.f;        // distances <= -reach, >= reach
     auto put = [&](int dist, float v) {
         if (dist >= reach) behind += v;
@@ -95,20 +94,21 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SBB : 1) soft
         turn ^= 1u;
         if (STAGES == 2) fetch_row(i + 1);      // the next row is on its way while this one is worked on
         ring.wait();
-        const int live = rows.live<NV>(end, c - 8 * rg.lane);
+        const int live = rows.live<NV>(end, warp_c);
         uint4 *ps = ring.place(turn ^ 1u, 0), *pd = ring.place(turn ^ 1u, 1);
-        with_blocks<NV>(live, [&](auto blocks) {
+        with_blocks<NV>(live, !a.causal, [&](auto blocks) {
             constexpr int L = decltype(blocks)::value;
+            if (end < warp_c + 256 * L) {
+                const int first = end > warp_c ? (int)((end - warp_c) / 256u) : 0;
+                ring.fill(ps, at, c, end, first, L, masked);
+                ring.fill(pd, at, c, end, first, L, 0u);
+            }
             float p[NV][8], g[L][8];
 #pragma unroll
             for (int k = 0; k < L; k++) {
                 ring.read(ps, k, at, p[k]);
                 ring.read(pd, k, at, g[k]);
                 add_bias(p[k], bias, reach, a.scale, (int)(rows.c0 + c + 256 * k) - pos);
-                if (k == L - 1) {               // (those before it are whole)
-                    mask_from(p[k], c + 256 * k, end, -INFINITY);
-                    mask_from(g[k], c + 256 * k, end, 0.f);
-                }
             }
             if constexpr (DROP) drop_row<L>(d, (u32)row, (rows.c0 + c) >> 3, g);      // (the factor comes where dp is used)
             exp_about<L>(p, lse == -INFINITY ? 0.f : lse);
@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? SBB : 1) soft
                     carry = from;
                 }
                 if (k < L) {
-                    mul8(p[k], a.scale);
+                    mul8(p[k], a.out_scale);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; e++) p[k][e] = 0.f;
@@ -273,20 +273,15 @@ template <u32 TYPE> static void launch_type(const SoftmaxArgs &a, cudaStream_t s
 // Sums by bucket of every CTA, and sums by distance of every warp where those do not fit into shared memory.
 size_t softmax_workspace(SoftmaxArgs &a)
 {
-    size_t most = 0;
-    for (int aligned = 0; aligned < 2; aligned++) {
-        softmax_split(a, true, aligned != 0);
-        const size_t ctas = (size_t)a.batch * a.heads * a.chunks * a.cluster;
-        const size_t lines = a.reach > kLineReach ? ctas * (a.tpr * a.groups / 32) * (2 * a.reach + 1) : 0;
-        const size_t bytes = (ctas * a.buckets + lines) * sizeof(float);
-        if (bytes > most) most = bytes;
-    }
-    return most;
+    softmax_split(a, true);
+    const size_t ctas = (size_t)a.batch * a.heads * a.chunks * a.cluster;
+    const size_t lines = a.reach > kLineReach ? ctas * (a.tpr * a.groups / 32) * (2 * a.reach + 1) : 0;
+    return (ctas * a.buckets + lines) * sizeof(float);
 }
 
 int launch_softmax_back(SoftmaxArgs &a, u32 type, cudaStream_t st)
 {
-    softmax_split(a, true, a.ld % 8u == 0);
+    softmax_split(a, true);
     if (!a.table || !a.dtable) a.partial = nullptr;
     const bool any = (u64)a.batch * a.heads * a.q_len != 0;
     if (any) {

@@ -113,6 +113,17 @@ def test_matches_definition(rows, cols, kind, param, fused, p):
     _check_backward(s, kind, param, fused)
 
 
+# enough rows for the kernels that give a thread several blocks of eight columns
+@pytest.mark.parametrize("rows,cols", [(1300, 264), (1203, 300), (1250, 512), (1190, 777), (1200, 1024), (1185, 1001),
+                                       (700, 2056), (650, 2047), (320, 4096), (400, 4100), (160, 8200), (150, 16387)])
+@pytest.mark.parametrize("kind,param,fused,p", [("f32", "f32", True, 0.1), ("bf16", "f32", True, 0.1),
+                                                 ("f16", "f16", False, 0.0)])
+def test_many_rows(rows, cols, kind, param, fused, p):
+    s = _case(rows, cols, kind, param, fused, p)
+    _check_forward(s, kind)
+    _check_backward(s, kind, param, fused)
+
+
 @pytest.mark.parametrize("cols", [64, 1001, 4096])
 def test_without_parameters_and_with_a_large_mean(cols):
     s = _case(12, cols, "f32", "f32", True, 0.1, affine=False, offset=1000.0)

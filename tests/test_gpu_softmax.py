@@ -134,6 +134,23 @@ def test_matches_definition(b, h, q, k, kind, causal, both, p, ragged):
     c.check_backward()
 
 
+@pytest.mark.parametrize("k", [70000, 70001, 131072])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_longest_rows(k, kind):
+    c = Case(1, 1, 2, k, kind, True, [k - 1000], 0.1)
+    c.check_forward()
+    c.check_backward()
+
+
+@pytest.mark.parametrize("b,h,q,k", [(1, 2, 130, 1024), (2, 2, 200, 997), (1, 1, 300, 1500), (1, 1, 90, 3001), (2, 1, 70, 4096)])
+@pytest.mark.parametrize("kind,causal,scale", [("bf16", True, -0.5), ("f32", False, 0.0), ("f16", True, 0.25), ("f32", True, 1.0)])
+def test_many_rows_and_scales(b, h, q, k, kind, causal, scale):
+    lens = None if causal else [k - 300] * b
+    c = Case(b, h, q, k, kind, causal, lens, 0.1, both=not causal, scale=scale)
+    c.check_forward()
+    c.check_backward()
+
+
 @pytest.mark.parametrize("k,pad", [(40, 8), (1000, 24), (37, 3), (61, 4), (2000, 0), (2001, 7), (33, 7)])
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 def test_rows_spaced_apart(k, pad, kind):
