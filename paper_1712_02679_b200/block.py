@@ -1,0 +1,151 @@
+"""The operators of a transformer block as differentiable functions: dropout, layer norm (alone, or behind a residual add
+and dropout) and the attention softmax with a learned relative position bias.
+
+Each call runs the library's kernels, forward and backward (binding.adacomp_dropout, adacomp_layer_norm*,
+adacomp_bias_softmax*; see include/adacomp.h); the parameters' gradients are what adacomp_compress* packs.
+
+Random masks are a function of (seed, step, site): `Rng` holds seed and step in device memory, `site` tells a model's
+dropouts apart.  No mask is stored: the backward pass draws it again, so the step must not move on between the two.
+"""
+from __future__ import annotations
+
+from typing import Optional
+
+import torch
+
+from . import binding as B
+
+__all__ = ["Rng", "dropout", "layer_norm", "add_layer_norm", "bias_softmax", "relpos"]
+
+relpos = B.adacomp_relpos_plan          # the buckets of a relative position bias
+
+
+class Rng:
+    """Seed and step of the model's dropouts."""
+
+    def __init__(self, seed: int, device="cuda"):
+        self.state = torch.tensor([seed, 0], dtype=torch.int64, device=device)
+
+    def advance(self) -> None:
+        """The next training step's masks (on the current stream; may be captured into a CUDA graph)."""
+        self.state[1] += 1
+
+
+def _mask_key(ctx, rng: Optional[Rng], p: float):
+    """The rng tensor of a call that draws, remembered with its version so that the backward pass can tell."""
+    if p == 0.0:
+        ctx.rng = None
+        return None
+    if rng is None:
+        raise ValueError("dropout needs an Rng")
+    ctx.rng, ctx.rng_version = rng.state, rng.state._version
+    return ctx.rng
+
+
+def _same_key(ctx):
+    if ctx.rng is not None and ctx.rng._version != ctx.rng_version:
+        raise RuntimeError("the Rng moved on between the forward and the backward pass: its masks are gone")
+    return ctx.rng
+
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, p, rng, site):
+        ctx.p, ctx.site = p, site
+        key = _mask_key(ctx, rng, p)
+        y = torch.empty_like(x)
+        B.adacomp_dropout(x, y, p, key, site)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        dx = torch.empty_like(dy, memory_format=torch.contiguous_format)
+        B.adacomp_dropout(dy.contiguous(), dx, ctx.p, _same_key(ctx), ctx.site)
+        return dx, None, None, None
+
+
+def dropout(x: torch.Tensor, p: float, rng: Rng, site: int = 0, training: bool = True) -> torch.Tensor:
+    """x with each element dropped with probability p (in steps of 2^-16) and the others scaled up."""
+    return _Dropout.apply(x.contiguous(), p, rng, site) if training and p > 0.0 else x
+
+
+class _Norm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, weight, bias, eps, p, rng, site):
+        ctx.p, ctx.site = p, site
+        key = _mask_key(ctx, rng, p)
+        stat = x.shape[:-1]
+        y = torch.empty_like(x)
+        mean, rstd = (torch.empty(stat, dtype=torch.float32, device=x.device) for _ in range(2))
+        fused = residual is not None or p > 0.0
+        h = torch.empty_like(x) if fused else x
+        B.adacomp_layer_norm(x, weight, bias, y, mean, rstd, eps, residual, h if fused else None, p, key, site)
+        ctx.save_for_backward(h, weight, mean, rstd)
+        ctx.has_residual, ctx.has_bias = residual is not None, bias is not None
+        return (y, h) if fused else y
+
+    @staticmethod
+    def backward(ctx, dy, dh=None):
+        h, weight, mean, rstd = ctx.saved_tensors
+        dx = torch.empty_like(h)
+        separate = ctx.has_residual and ctx.p > 0.0
+        dres = torch.empty_like(h) if separate else None
+        dweight = torch.empty_like(weight) if weight is not None and ctx.needs_input_grad[2] else None
+        kind = weight.dtype if weight is not None else torch.float32
+        dbias = torch.empty(h.shape[-1:], dtype=kind, device=h.device) if ctx.has_bias and ctx.needs_input_grad[3] else None
+        workspace = None
+        if dweight is not None or dbias is not None:
+            rows = h.numel() // h.shape[-1]
+            workspace = torch.empty(B.adacomp_layer_norm_workspace(rows, h.shape[-1]), dtype=torch.uint8, device=h.device)
+        B.adacomp_layer_norm_backward(dy.contiguous(), h, weight, mean, rstd, dx, dweight, dbias, workspace,
+                                      dh.contiguous() if dh is not None else None, dres, ctx.p, _same_key(ctx), ctx.site)
+        return dx, (dres if separate else dx) if ctx.has_residual else None, dweight, dbias, None, None, None, None
+
+
+def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor],
+               eps: float = 1e-5) -> torch.Tensor:
+    """Layer norm over the last dimension; weight and bias float32 or of x's type."""
+    return _Norm.apply(x.contiguous(), None, weight, bias, eps, 0.0, None, 0)
+
+
+def add_layer_norm(x: torch.Tensor, residual: torch.Tensor, weight, bias, p: float = 0.0, rng: Optional[Rng] = None,
+                   site: int = 0, eps: float = 1e-5, training: bool = True):
+    """(layer_norm(h), h) with h = residual + dropout(x), in one pass forward and one backward."""
+    return _Norm.apply(x.contiguous(), residual.contiguous(), weight, bias, eps, p if training else 0.0, rng, site)
+
+
+class _BiasSoftmax(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, scores, table, plan, scale, causal, q_offset, key_len, p, rng, site):
+        key = _mask_key(ctx, rng, p)
+        probs = torch.empty_like(scores)
+        lse = torch.empty(scores.shape[:3], dtype=torch.float32, device=scores.device)
+        ctx.call = dict(scale=scale, causal=causal, q_offset=q_offset, p=p, site=site)
+        ctx.plan = plan
+        B.adacomp_bias_softmax(scores, table, plan, probs, lse, key_len=key_len, rng=key, **ctx.call)
+        ctx.save_for_backward(scores, table, lse, key_len)
+        return probs
+
+    @staticmethod
+    def backward(ctx, dprobs):
+        scores, table, lse, key_len = ctx.saved_tensors
+        dscores = torch.empty_like(scores)
+        dtable = workspace = None
+        if table is not None and ctx.needs_input_grad[1]:
+            dtable = torch.empty_like(table)
+            workspace = torch.empty(B.adacomp_bias_softmax_workspace(*scores.shape, ctx.plan), dtype=torch.uint8,
+                                    device=scores.device)
+        B.adacomp_bias_softmax_backward(dprobs.contiguous(), scores, table, ctx.plan, lse, dscores, dtable, workspace,
+                                        key_len=key_len, rng=_same_key(ctx), **ctx.call)
+        return dscores, dtable, None, None, None, None, None, None, None, None
+
+
+def bias_softmax(scores: torch.Tensor, table: Optional[torch.Tensor], plan, scale: float = 1.0, causal: bool = False,
+                 q_offset: Optional[int] = None, key_len: Optional[torch.Tensor] = None, p: float = 0.0,
+                 rng: Optional[Rng] = None, site: int = 0, training: bool = True) -> torch.Tensor:
+    """Attention probabilities of scores [batch, heads, queries, keys] with table [buckets, heads] added by distance.
+    q_offset: position of the first query among the keys (None: the queries are the last positions)."""
+    if q_offset is None:
+        q_offset = scores.shape[3] - scores.shape[2]
+    return _BiasSoftmax.apply(scores.contiguous(), table, plan, scale, causal, q_offset, key_len, p if training else 0.0, rng,
+                              site)
