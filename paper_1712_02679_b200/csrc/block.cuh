@@ -260,13 +260,13 @@ __device__ inline void mask_from(float (&v)[8], u32 c, u32 end, float fill)
     }
 }
 
-// Stores the block's columns before `cols`.  Unless ALIGNED, all lanes of the warp take part, with neighbouring blocks.
+// Stores the block's columns before `cols`.  Unless ALIGNED, all lanes of the warp take part; where a lane's block is not a
+// row's first, the lane before it holds the block before it.
 template <u32 TYPE, bool ALIGNED>
 __device__ inline void store_block(void *base, u64 row_at, u32 c, u32 cols, const float (&v)[8])
 {
     constexpr u32 per = chunk_elems<TYPE>();
-    const u32 s = ALIGNED ? 0u : (u32)row_at & (per - 1u);
-    if (ALIGNED || s == 0u) {
+    if constexpr (ALIGNED) {
         if (c + 8 <= cols) store8<TYPE>(base, row_at + c, narrow8<TYPE>(v));
         if (cols & 7u) {                // (what lies behind the row's last column is not this row's)
             if (c < cols && c + 8 > cols) {
@@ -277,12 +277,13 @@ __device__ inline void store_block(void *base, u64 row_at, u32 c, u32 cols, cons
         }
         return;
     }
+    const u32 s = (u32)row_at & (per - 1u);
     const u32 lane = threadIdx.x & 31u;
     const Vec8<TYPE> mine8 = narrow8<TYPE>(v);
     const u32 *n = reinterpret_cast<const u32 *>(mine8.q);
     uint4 *p = reinterpret_cast<uint4 *>(static_cast<unsigned char *>(base) + (row_at + c - s) * type_size(TYPE));
-    const bool first = lane > 0u && c + per - s <= cols;            // the chunk that starts with the neighbour's elements
-    const bool next = lane < 31u && c + 8u + per - s <= cols;       // the chunk the next lane completes with mine
+    const bool first = (s == 0u || (lane > 0u && c > 0u)) && c + per - s <= cols;    // the chunk that starts with the neighbour's elements
+    const bool next = s == 0u || (lane < 31u && c + 8u + per - s <= cols);           // the chunk the next lane completes with mine
     if constexpr (TYPE == ADACOMP_TYPE_F32) {
         u32 in[12], out[8];
 #pragma unroll
@@ -290,6 +291,8 @@ __device__ inline void store_block(void *base, u64 row_at, u32 c, u32 cols, cons
 #pragma unroll
         for (int i = 0; i < 8; i++) in[4 + i] = n[i];
         shift_words<8>(in, 4u - s, out);
+#pragma unroll
+        for (int i = 0; i < 8; i++) out[i] = s ? out[i] : n[i];
         const bool second = c + 8u - s <= cols;
         if (first) p[0] = make_uint4(out[0], out[1], out[2], out[3]);
         if (second) p[1] = make_uint4(out[4], out[5], out[6], out[7]);
@@ -308,7 +311,7 @@ __device__ inline void store_block(void *base, u64 row_at, u32 c, u32 cols, cons
         shift_words<5>(in, (8u - s) >> 1, y);
         u32 out[4];
 #pragma unroll
-        for (int i = 0; i < 4; i++) out[i] = __funnelshift_r(y[i], y[i + 1], (s & 1u) * 16u);
+        for (int i = 0; i < 4; i++) out[i] = s ? __funnelshift_r(y[i], y[i + 1], (s & 1u) * 16u) : n[i];
         if (first) p[0] = make_uint4(out[0], out[1], out[2], out[3]);
         if (!(first && next)) {
 #pragma unroll

@@ -28,6 +28,10 @@ inline void launch_after(void (*kernel)(P...), dim3 grid, unsigned threads, cuda
     cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+// Threads of a CTA that adds up `lines` lines of numbers, 32 columns of them: a warp for every two lines.
+constexpr int kSumWarps = 32;
+inline unsigned sum_threads(u64 lines) { return 32u * (unsigned)(lines >= 2 * kSumWarps ? kSumWarps : (lines + 1) / 2 ? (lines + 1) / 2 : 1); }
+
 int launched();        // ADACOMP_OK, or ADACOMP_ERR_CUDA when the last launch failed
 
 // dropout.cu

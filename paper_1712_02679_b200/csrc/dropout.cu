@@ -40,33 +40,31 @@ dropout_wide(const void *x, void *y, u32 row0, u32 n_groups, FastDiv per_row, Dr
     }
 }
 
-// Any row length: a warp takes 256 columns of a row at a time.
+// Any row length: the tensor is one line of blocks of up to eight columns, row after row; a warp takes 32 of them at a time.
 template <u32 TYPE>
 __global__ void __launch_bounds__(kDropThreads)
-dropout_any(const void *x, void *y, u32 row0, u32 n_items, u32 cols, FastDiv per_row, DropArgs args)
+dropout_any(const void *x, void *y, u32 row0, u32 n_blocks, u32 cols, FastDiv per_row, DropArgs args)
 {
     const Drop d = drop_begin(args);
-    const u32 lane = threadIdx.x & 31u;
-    const u32 item0 = blockIdx.x * (kDropThreads / 32 * kDropAnyPer) + (threadIdx.x >> 5);
+    const u32 b0 = blockIdx.x * (kDropThreads * kDropAnyPer) + threadIdx.x;
     Raw<TYPE, false> raw[kDropAnyPer];
+    u32 row[kDropAnyPer], group[kDropAnyPer], w[kDropAnyPer][4];
 #pragma unroll
     for (int i = 0; i < kDropAnyPer; i++) {
-        const u32 item = item0 + i * (kDropThreads / 32);
-        const u32 r = fast_div(item, per_row), c = ((item - r * per_row.d) * 32u + lane) * 8u;
-        if (item < n_items) fetch<TYPE, false>(raw[i], x, ((u64)row0 + r) * cols, c, cols);
+        const u32 b = b0 + i * kDropThreads, r = fast_div(b, per_row);
+        row[i] = row0 + r;
+        group[i] = b - r * per_row.d;
+        if (b < n_blocks) fetch<TYPE, false>(raw[i], x, (u64)row[i] * cols, group[i] * 8u, cols);
     }
+    drop_words<kDropAnyPer>(d, row, group, w);
 #pragma unroll
     for (int i = 0; i < kDropAnyPer; i++) {
-        const u32 item = item0 + i * (kDropThreads / 32);
-        if (item >= n_items) break;
-        const u32 r = fast_div(item, per_row), c = ((item - r * per_row.d) * 32u + lane) * 8u;
-        const u64 at = ((u64)row0 + r) * cols;
+        const bool there = b0 + i * kDropThreads < n_blocks;
+        const u64 at = (u64)row[i] * cols;
         float v[8];
         unpack<TYPE, false>(raw[i], at, v);
-        u32 w[4];
-        drop_words(d, row0 + r, c >> 3, w);
-        drop_apply(d, w, v);
-        store_block<TYPE, false>(y, at, c, cols, v);
+        drop_apply(d, w[i], v);
+        store_block<TYPE, false>(y, at, there ? group[i] * 8u : cols, cols, v);
     }
 }
 
@@ -74,7 +72,7 @@ template <u32 TYPE>
 static void launch_type(const void *x, void *y, u64 rows, u32 cols, const DropArgs &drop, cudaStream_t st)
 {
     const bool wide = cols % 8u == 0;
-    const u32 per_row = wide ? cols / 8u : (cols + 255u) / 256u;
+    const u32 per_row = (cols + 7u) / 8u;
     const FastDiv f = make_fastdiv(per_row);
     const u64 slice = 0x7fffffffu / per_row;         // rows a launch covers: items are numbered in 31 bits
     for (u64 row0 = 0; row0 < rows; row0 += slice) {
@@ -83,7 +81,7 @@ static void launch_type(const void *x, void *y, u64 rows, u32 cols, const DropAr
             const u32 per_cta = kDropThreads * kDropPer;
             dropout_wide<TYPE><<<(items - 1) / per_cta + 1, kDropThreads, 0, st>>>(x, y, (u32)row0, items, f, drop);
         } else {
-            const u32 per_cta = kDropThreads / 32 * kDropAnyPer;
+            const u32 per_cta = kDropThreads * kDropAnyPer;
             dropout_any<TYPE><<<(items - 1) / per_cta + 1, kDropThreads, 0, st>>>(x, y, (u32)row0, items, cols, f, drop);
         }
     }

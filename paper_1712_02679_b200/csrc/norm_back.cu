@@ -166,8 +166,6 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? 2 : 1) norm_ba
     }
 }
 
-constexpr int kSumWarps = 32;
-
 // dweight (blockIdx.y = 0) and dbias: 32 columns per CTA, the CTAs' lines in a fixed order.
 __global__ void __launch_bounds__(32 * kSumWarps) norm_back_sum(const float *partial, u32 partials, u32 cols, void *dweight,
                                                                void *dbias, u32 param_type)
@@ -175,20 +173,19 @@ __global__ void __launch_bounds__(32 * kSumWarps) norm_back_sum(const float *par
     __shared__ float sums[kSumWarps][33];
     void *out = blockIdx.y ? dbias : dweight;
     if (!out) return;
-    const u32 lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, c = blockIdx.x * 32u + lane;
+    const u32 lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, c = blockIdx.x * 32u + lane, warps = blockDim.x >> 5;
     wait_for_kernel_before();
     float s = 0.f;
     if (c < cols) {
         const float *p = partial + (u64)blockIdx.y * cols + c;
 #pragma unroll 10
-        for (u32 i = warp; i < partials; i += kSumWarps) s += p[(u64)i * 2 * cols];
+        for (u32 i = warp; i < partials; i += warps) s += p[(u64)i * 2 * cols];
     }
     sums[warp][lane] = s;
     __syncthreads();
     if (warp != 0 || c >= cols) return;
     s = 0.f;
-#pragma unroll
-    for (int i = 0; i < kSumWarps; i++) s += sums[i][lane];
+    for (u32 i = 0; i < warps; i++) s += sums[i][lane];
     if (param_type == ADACOMP_TYPE_F32) store1<ADACOMP_TYPE_F32>(out, c, s);
     else if (param_type == ADACOMP_TYPE_BF16) store1<ADACOMP_TYPE_BF16>(out, c, s);
     else store1<ADACOMP_TYPE_F16>(out, c, s);
@@ -224,7 +221,7 @@ int launch_norm_back(NormArgs &a, u32 type, cudaStream_t st)
         else launch_type<ADACOMP_TYPE_F16>(a, st);
     }
     if (a.partial)
-        launch_after(norm_back_sum, dim3((a.cols + 31u) / 32u, 2), 32 * kSumWarps, st, (const float *)a.partial,
+        launch_after(norm_back_sum, dim3((a.cols + 31u) / 32u, 2), sum_threads(a.sets), st, (const float *)a.partial,
                      a.rows ? a.sets : 0u, a.cols, a.dweight, a.dbias, a.param_type);
     return launched();
 }

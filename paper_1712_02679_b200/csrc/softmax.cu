@@ -36,7 +36,7 @@ void softmax_split(SoftmaxArgs &a, bool back)
     // which costs it about `fixed` rows' work; against that stands the end of the launch, where about one CTA's work is
     // spent on an emptying GPU.
     const u64 fixed = back ? 4 : 2, heads = (u64)a.batch * a.heads;
-    const u64 slots = (u64)kBlockSms * (back ? 12 : 16) * 32 / (a.tpr * a.groups);
+    const u64 slots = (u64)kBlockSms * (a.threads == kSoftShort ? soft_ctas((int)a.per, back) * kSoftShort : kSoftThreads) / (a.tpr * a.groups);
     u64 best = ~0ull;
     a.run = 1;
     const u32 longest = (a.q_len + a.groups - 1) / a.groups;
@@ -51,7 +51,7 @@ void softmax_split(SoftmaxArgs &a, bool back)
 // A row stays in registers.  Each warp takes powers of two about its own maximum; the maxima and sums of the row's warps
 // are joined in one meeting, and what a warp holds is rescaled as it is stored.
 template <u32 TYPE, bool ALIGNED, int NV, bool DROP, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? 4 : 1) softmax_forward(const SoftmaxArgs a)
+__global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? soft_ctas(NV, false) : 1) softmax_forward(const SoftmaxArgs a)
 {
     extern __shared__ uint4 dynamic[];
     __shared__ unsigned short first[ADACOMP_MAX_BUCKETS];

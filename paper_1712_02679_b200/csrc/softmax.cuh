@@ -9,6 +9,9 @@ namespace cg = cooperative_groups;
 
 constexpr int kSoftThreads = 512;            // most threads of a CTA
 constexpr int kSoftShort = 128;              // threads of a CTA whose rows are one warp each
+// CTAs of short rows that an SM holds, by blocks per lane: what the registers of each kernel are held down to.
+__host__ __device__ constexpr int soft_ctas(int nv, bool back) { return back ? (nv == 1 ? 5 : nv == 2 ? 4 : 3) : nv == 1 ? 8 : nv == 2 ? 5 : 4; }
+
 // Reach up to which the backward pass keeps its sums by distance in shared memory: with more, 16 warps' lines, the rows on
 // their way and the bias would not fit beside one another, and the lines lie behind the CTAs' sums in the workspace.
 constexpr u32 kLineReach = 200;
@@ -22,14 +25,15 @@ __device__ inline float exp2_fast(float x)
     return y;
 }
 
-// v = e^(v - about) in the first L blocks, about not -inf.  The product with log2(e) is taken of the difference: that of a
-// type's lowest value (a mask added by the caller) would overflow, and rows of nothing else keep their softmax this way.
+// v = e^(v - about) in the first L blocks, about not -inf: 2^(v log2(e) - about log2(e)).  Where the product of `about`
+// would overflow (rows of a type's lowest value, a mask added by the caller), neighbouring numbers are 2^103 apart and the
+// exponential is 1 for v = about and 0 for anything smaller; a power of two in the place of log2(e) gives just that.
 template <int L, int NV> __device__ inline void exp_about(float (&v)[NV][8], float about)
 {
+    const float unit = fabsf(about) < 1e38f ? kLog2e : 0x1p-93f, shift = -about * unit;
 #pragma unroll
     for (int k = 0; k < L; k++) {
-        add8(v[k], -about);
-        mul8(v[k], kLog2e);
+        fma8(v[k], unit, shift);
 #pragma unroll
         for (int e = 0; e < 8; e++) v[k][e] = exp2_fast(v[k][e]);
     }

@@ -17,7 +17,7 @@ namespace adacomp_impl {
 __host__ __device__ constexpr int soft_back_stages(int nv, int threads) { return nv == 4 && threads == kSoftThreads ? 1 : 2; }
 
 template <u32 TYPE, bool ALIGNED, int NV, bool DROP, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? 3 : 1) softmax_backward(const SoftmaxArgs a)
+__global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? soft_ctas(NV, true) : 1) softmax_backward(const SoftmaxArgs a)
 {
     extern __shared__ uint4 dynamic[];
     __shared__ unsigned short first[ADACOMP_MAX_BUCKETS];
@@ -218,19 +218,20 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? 3 : 1) softma
     }
 }
 
-constexpr int kTableSumWarps = 32;
+constexpr int kTableSumWarps = kSumWarps;
 
 // dtable[b][head]: the sums of that head's CTAs (`per` of each sequence's), in their order.
 __global__ void __launch_bounds__(32 * kTableSumWarps)
 softmax_back_sum(const float *partial, float *dtable, u32 batch, u32 heads, u32 per, u32 buckets)
 {
     __shared__ float sums[kTableSumWarps][33];
-    const u32 head = blockIdx.x, lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, b = blockIdx.y * 32u + lane;
+    const u32 head = blockIdx.x, lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, b = blockIdx.y * 32u + lane,
+              warps = blockDim.x >> 5;
     wait_for_kernel_before();
     float s = 0.f;
     if (b < buckets) {
 #pragma unroll 8
-        for (u64 j = warp; j < (u64)batch * per; j += kTableSumWarps) {
+        for (u64 j = warp; j < (u64)batch * per; j += warps) {
             const u64 n = j / per;
             s += partial[((n * heads + head) * per + (j - n * per)) * buckets + b];
         }
@@ -239,8 +240,7 @@ softmax_back_sum(const float *partial, float *dtable, u32 batch, u32 heads, u32 
     __syncthreads();
     if (warp != 0 || b >= buckets) return;
     s = 0.f;
-#pragma unroll
-    for (int w = 0; w < kTableSumWarps; w++) s += sums[w][lane];
+    for (u32 w = 0; w < warps; w++) s += sums[w][lane];
     dtable[(u64)b * heads + head] = s;
 }
 
@@ -290,7 +290,7 @@ int launch_softmax_back(SoftmaxArgs &a, u32 type, cudaStream_t st)
         else launch_type<ADACOMP_TYPE_F16>(a, st);
     }
     if (a.table && a.dtable && a.heads)
-        launch_after(softmax_back_sum, dim3(a.heads, (a.buckets + 31u) / 32u), 32 * kTableSumWarps, st, (const float *)a.partial,
+        launch_after(softmax_back_sum, dim3(a.heads, (a.buckets + 31u) / 32u), sum_threads((u64)a.batch * a.chunks * a.cluster), st, (const float *)a.partial,
                      a.dtable, any ? a.batch : 0u, a.heads, a.chunks * a.cluster, a.buckets);
     return launched();
 }
