@@ -1,5 +1,12 @@
 // Dropout from a counter-based generator: y = keep ? x * factor : 0, the mask recomputed wherever it is needed and never
 // stored.  Its backward pass is the same map applied to dy.
+//
+// Bound by memory, x in and y out, with the generator close behind: ten rounds are 20 products of 32 bits and as many
+// exclusive ors for eight elements, which is why an element takes 16 bits of them and not 32 (with 32 the 16-bit types would
+// be bound by the generator), and why the blocks of a thread go through the rounds together and share the key's additions
+// (47 -> 42 us).  16384 x 4096 bf16: 41.7 us, 6.43 TB/s, 98 % of the measured copy rate; rows that start anywhere, 24336 x
+// 313 binary16: 13 us (0.36 of it), bound by the shifting (19 us with a warp per 256 columns of a row: most lanes of a short
+// row's second warp were idle).
 #include "block.h"
 
 namespace adacomp_impl {

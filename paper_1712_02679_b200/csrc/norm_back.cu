@@ -1,5 +1,11 @@
 // Layer norm, backward: the gradient of h (to the residual, and through dropout to x), and the weight's and bias's
 // gradients, which are sums over all rows.
+//
+// Read once, written once: dy, h (and dh_in) in, dx (and dresidual) out, one pass for the rows' sums and the columns'.
+// 16 columns per thread keep both column sums, 32 numbers, in registers; more would spill, fewer (8) let the row's meeting
+// dominate (120 us against 141, 16384 x 4096 bf16 with residual and dropout).  That case: 120 us, 0.85 of the measured copy
+// rate, of which the second kernel's lines are 4 us.  8192 x 1024: 16 us (0.47): 14 rows per group of threads, against which
+// the launch of two kernels, the parameters and the adding of 296 lines stand.  777 x 1001 binary32: 12 us, latency.
 #include "norm.cuh"
 
 namespace adacomp_impl {
@@ -185,6 +191,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) norm_back_sum(const float *par
     __syncthreads();
     if (warp != 0 || c >= cols) return;
     s = 0.f;
+#pragma unroll 8
     for (u32 i = 0; i < warps; i++) s += sums[i][lane];
     if (param_type == ADACOMP_TYPE_F32) store1<ADACOMP_TYPE_F32>(out, c, s);
     else if (param_type == ADACOMP_TYPE_BF16) store1<ADACOMP_TYPE_BF16>(out, c, s);

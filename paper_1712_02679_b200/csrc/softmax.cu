@@ -1,5 +1,13 @@
 // Attention softmax with a learned relative position bias by buckets, forward: from scores to probabilities, with the
 // scale, the causal and length masks and dropout, in one pass.
+//
+// Read once, written once.  Bound by issued instructions, not by memory: with dropout a kept element costs 23 of them (8 the
+// generator and its comparisons, 2 the exponential), at 65 % of the issue slots; without dropout 15.  8 x 16 x 1024 x 1024
+// bf16, dropout: 129 us with all keys kept (0.63 of the measured copy rate; 97 us without dropout, 0.85), 132 us with ragged
+// lengths (0.54).  What made it: 32 keys per lane and no meeting up to 1024 keys (two warps a row with 16: 168 us), the bias
+// by two 16-byte reads per eight keys instead of eight reads and clamps, masks written into the row before the arithmetic,
+// blocks behind a row's end left out.  One token, 16 x 16 rows of 16384: 10 us, two waves of CTAs of one row each, where
+// the latency of load, laying out the bias, meeting and store shows.
 #include "softmax.cuh"
 
 namespace adacomp_impl {
