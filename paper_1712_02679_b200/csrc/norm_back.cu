@@ -184,8 +184,13 @@ __global__ void __launch_bounds__(32 * kSumWarps) norm_back_sum(const float *par
     float s = 0.f;
     if (c < cols) {
         const float *p = partial + (u64)blockIdx.y * cols + c;
-#pragma unroll 10
-        for (u32 i = warp; i < partials; i += warps) s += p[(u64)i * 2 * cols];
+        for (u32 i0 = warp; i0 < partials; i0 += 8 * warps) {       // eight lines on their way at a time
+            float x[8];
+#pragma unroll
+            for (u32 j = 0; j < 8; j++) x[j] = i0 + j * warps < partials ? p[(u64)(i0 + j * warps) * 2 * cols] : 0.f;
+#pragma unroll
+            for (u32 j = 0; j < 8; j++) s += x[j];
+        }
     }
     sums[warp][lane] = s;
     __syncthreads();

@@ -238,10 +238,16 @@ softmax_back_sum(const float *partial, float *dtable, u32 batch, u32 heads, u32 
     wait_for_kernel_before();
     float s = 0.f;
     if (b < buckets) {
-#pragma unroll 8
-        for (u64 j = warp; j < (u64)batch * per; j += warps) {
-            const u64 n = j / per;
-            s += partial[((n * heads + head) * per + (j - n * per)) * buckets + b];
+        const u32 lines = batch * per;          // (each a CTA, so their number has 31 bits)
+        for (u32 i0 = warp; i0 < lines; i0 += 8 * warps) {          // eight on their way at a time
+            float x[8];
+#pragma unroll
+            for (u32 j = 0; j < 8; j++) {
+                const u32 i = i0 + j * warps, n = i / per;
+                x[j] = i < lines ? partial[(((u64)n * heads + head) * per + (i - n * per)) * buckets + b] : 0.f;
+            }
+#pragma unroll
+            for (u32 j = 0; j < 8; j++) s += x[j];
         }
     }
     sums[warp][lane] = s;
