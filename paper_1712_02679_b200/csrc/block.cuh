@@ -482,30 +482,28 @@ template <u32 TYPE, bool ALIGNED, int NV, int THREADS, int STAGES> struct Ring {
             for (int i = 0; i < kChunks; i++) line[at(k, i)] = r.q[i];
         }
         __syncwarp();
+        // The warp's columns are first .. end - 1.  Chunks that lie inside them are stored whole, by the lane whose block
+        // begins in them ...
+        const u32 first = c - 8u * lane, end = min(cols, first + 256u * NV);
         unsigned char *p = static_cast<unsigned char *>(to) + (row_at + c - s) * type_size(TYPE);
 #pragma unroll
         for (int k = 0; k < NV; k++) {
-            // what lies s elements before the block is whole chunks; the warp's first one starts in another warp's columns
-            const u32 ck = c + 256 * k;
             Vec8<TYPE> r;
             read_at<TYPE>(line + at(k, 0) - 1, kPer - s, r);
-            const bool inside = k > 0 || lane > 0u;
-            bool whole = true;
 #pragma unroll
-            for (int i = 0; i < kChunks; i++) {
-                const bool full = (i > 0 || inside) && ck + (i + 1) * kPer - s <= cols;
-                if (full) *reinterpret_cast<uint4 *>(p + (256 * k + i * kPer) * type_size(TYPE)) = r.q[i];
-                whole = whole && full;
-            }
-            const bool next = (k + 1 < NV || lane < 31u) && ck + 8u + kPer - s <= cols;     // takes this block's last elements
-            if (!(whole && next)) {
-#pragma unroll
-                for (u32 e = 0; e < 8; e++) {
-                    // element e lies in chunk (e + s) / kPer of the block's chunks, the last of which is the next block's
-                    const u32 chunk = (e + s) / kPer;
-                    const bool done = chunk == (u32)kChunks ? next : (chunk > 0u || inside) && ck + (chunk + 1) * kPer - s <= cols;
-                    if (ck + e < cols && !done) store1<TYPE>(to, row_at + ck + e, v[k][e]);
-                }
+            for (int i = 0; i < kChunks; i++)
+                if ((k > 0 || i > 0 || lane > 0u) && c + 256 * k + (i + 1) * kPer - s <= end)
+                    *reinterpret_cast<uint4 *>(p + (256 * k + i * kPer) * type_size(TYPE)) = r.q[i];
+        }
+        // ... and the few elements before the first and behind the last of them one by one, a lane each.
+        if (first < end) {
+            const u32 from = min(first + kPer - s, end), behind = from + (end - from) / kPer * kPer;
+            const u32 col = lane < 8u ? first + lane : behind + lane - 8u;
+            if (lane < 16u && (lane < 8u ? col < from : col < end)) {
+                const unsigned char *q = reinterpret_cast<const unsigned char *>(line - lane * kChunks) + (col - first) * type_size(TYPE);
+                unsigned char *g = static_cast<unsigned char *>(to) + (row_at + col) * type_size(TYPE);
+                if (TYPE == ADACOMP_TYPE_F32) *reinterpret_cast<u32 *>(g) = *reinterpret_cast<const u32 *>(q);
+                else *reinterpret_cast<unsigned short *>(g) = *reinterpret_cast<const unsigned short *>(q);
             }
         }
     }
