@@ -5,7 +5,7 @@
 // elements.  So threads hold up to 32 columns each (49 us against 80 with 8, 16384 x 2048 bf16 with residual and dropout),
 // arithmetic goes in pairs, and the next row is copied past the registers while this one is worked on (without room for it
 // in registers: 144 us).  That case: 49 us, 0.83 of the measured copy rate.  Four rows of 4096: 3.0 us, launch and latency.
-// 5000 x 1001 binary16, rows that start anywhere: 11.5 us (0.27), two or three rows per warp and the shifting.
+// 5000 x 1001 binary16, rows that start anywhere: 11 us (0.28), two or three rows per warp and the shifting.
 #include "norm.cuh"
 
 namespace adacomp_impl {

@@ -3,10 +3,11 @@
 // Read once, written once: scores and dprobs in, dscores out; P is formed again from the scores, nothing but the row's
 // statistic is kept from the forward pass.  Bound by issued instructions at three CTAs per SM (P, dp and the diagonals' sums
 // are 96 registers at 32 keys per lane).  8 x 16 x 1024 x 1024 bf16, dropout: 172 us with all keys kept (0.71 of the measured
-// copy rate), 191 us with ragged lengths (0.54), 196 us causal (0.42: masked halves of a block are worked on, and rows of
+// copy rate), 190 us with ragged lengths (0.54), 196 us causal (0.42: masked halves of a block are worked on, and rows of
 // different lengths share an SM's instruction cache).  Sums by distance through shared memory, a read, an addition and a
-// write per element near the diagonal, had it at 331 us.  Odd causal rows, 3 x 8 x 997 x 997 binary16: 69 us (0.21): 24
-// heads give each warp few rows between laying out the bias and handing over its sums.
+// write per element near the diagonal, had it at 331 us.  Odd causal rows, 3 x 8 x 997 x 997 binary16: 58 us (0.25): 24
+// heads give each warp few rows between laying out the bias and handing over its sums, and unaligned rows cost half as much
+// again (4 x 8 x 1001 x 1001 bf16 84 us, 1000 x 1000 56 us).
 #include "softmax.cuh"
 
 namespace adacomp_impl {
