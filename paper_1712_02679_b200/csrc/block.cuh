@@ -702,6 +702,15 @@ template <int N> __device__ inline void row_sums(float (&v)[N], const RowGroup &
     for (int i = 0; i < N; i++) v[i] = from_lane(x, i * (int)span);
 }
 
+// The CTAs of a cluster meet; what threads 0 .. 31 wrote to one another's shared memory before is seen by all after.  (Only
+// they release: a release waits for all the thread's stores, those of the last row among them.)
+__device__ inline void cluster_meet()
+{
+    if (threadIdx.x < 32u) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    else asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
 // n / d for n < 2^31 by a multiplication (Granlund and Montgomery, "Division by invariant integers using
 // multiplication", 1994)
 struct FastDiv {

@@ -12,8 +12,9 @@ namespace adacomp_impl {
 
 // How a row's columns are shared.  Few rows: one thread per eight columns, up to 512 of them, for a short way through the
 // row.  Enough rows to give every SM `kNormBusy` warps of the other kind: threads with more columns each, up to `most`
-// blocks of eight, so that what a row costs besides its elements is shared by many of them.  Wider rows take a cluster of
-// CTAs.
+// blocks of eight, so that what a row costs besides its elements is shared by many of them (5000 x 1001 f16: 11 us against
+// 16; at 777 rows, below the bound, both alike).  Wider rows take CTAs of 512 threads with 16 columns each, then a cluster of
+// up to 8 CTAs (300 x 5000 bf16 backward: 11.6 us in one CTA a row, 13.7 in a cluster of two).
 void norm_split(NormArgs &a, u32 most)
 {
     const u32 blocks = (a.cols + 7u) / 8u;
@@ -22,7 +23,8 @@ void norm_split(NormArgs &a, u32 most)
     const u32 warps = (blocks + per * 32u - 1) / (per * 32u);
     const bool many = per > 1 && a.rows * warps >= (u64)kBlockSms * kNormBusy;
     a.per = many ? per : 1u;
-    const u32 cta = many ? kNormMany : kNormThreads;
+    const u32 cta = many && blocks <= kNormMany * per ? kNormMany : kNormThreads;       // (larger ones before a cluster)
+    if (many && cta == (u32)kNormThreads) a.per = 2u;
     a.cluster = 1;
     while (a.cluster < 8u && blocks > a.cluster * cta * a.per) a.cluster *= 2;
     if (blocks > a.cluster * cta * a.per) a.per = 2u;        // (only beyond 32768 columns)
@@ -49,7 +51,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? 2 : 1) norm_fo
     const u32 c0 = rank * a.slice, cols = min(a.slice, a.cols - c0);
     const u32 c = block_column<NV>(0, rg.t);                // block k starts at c + 256 k
     const bool res = a.residual != nullptr;
-    constexpr int STAGES = norm_stages(NV, THREADS);
+    constexpr int STAGES = norm_stages(NV, THREADS, TYPE);
     const Ring<TYPE, ALIGNED, NV, THREADS, STAGES> ring(dynamic, res ? 2u : 1u);
     float4 *params = reinterpret_cast<float4 *>(ring.end());
     const u64 step = (u64)a.sets * a.groups, step_at = step * a.cols;
@@ -95,7 +97,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? 2 : 1) norm_fo
         if (a.cluster > 1) {
             cg::cluster_group cl = cg::this_cluster();
             if (threadIdx.x < a.cluster) cl.map_shared_rank(&peers[parity][0], threadIdx.x)[rank] = v[0];
-            cl.sync();
+            cluster_meet();
             v[0] = 0.f;
             for (u32 j = 0; j < a.cluster; j++) v[0] += peers[parity][j];
         }
@@ -177,7 +179,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? 2 : 1) norm_fo
 
 template <u32 TYPE, bool ALIGNED, int NV, int THREADS> static void launch_drop(const NormArgs &a, cudaStream_t st)
 {
-    const size_t smem = Ring<TYPE, ALIGNED, NV, THREADS, norm_stages(NV, THREADS)>::bytes(a.residual ? 2u : 1u) + (NV == 1 ? 0 : (size_t)a.tpr * NV * 64);
+    const size_t smem = Ring<TYPE, ALIGNED, NV, THREADS, norm_stages(NV, THREADS, TYPE)>::bytes(a.residual ? 2u : 1u) + (NV == 1 ? 0 : (size_t)a.tpr * NV * 64);
     if (a.drop.threshold) launch_norm_kernel(norm_forward<TYPE, ALIGNED, NV, true, THREADS>, a, smem, st);
     else launch_norm_kernel(norm_forward<TYPE, ALIGNED, NV, false, THREADS>, a, smem, st);
 }

@@ -11,8 +11,12 @@ constexpr int kNormThreads = 512;            // most threads of a CTA
 constexpr int kNormMany = 256;               // threads of a CTA where there are many rows
 constexpr u32 kNormBusy = 8;                 // warps per SM that make many rows of them
 
-// Rows that are copied ahead (see Ring): rows beyond 32768 columns leave no room for a second one.
-__host__ __device__ constexpr int norm_stages(int nv, int threads) { return nv == 2 && threads == kNormThreads ? 1 : 2; }
+// Rows that are copied ahead (see Ring): three arrays of binary32 rows of 16 columns per thread leave no room for a second
+// row where a CTA has all 512 threads.
+__host__ __device__ constexpr int norm_stages(int nv, int threads, u32 type)
+{
+    return nv == 2 && threads == kNormThreads && type == ADACOMP_TYPE_F32 ? 1 : 2;
+}
 
 template <typename K> inline void launch_norm_kernel(K kernel, const NormArgs &a, size_t smem, cudaStream_t st)
 {

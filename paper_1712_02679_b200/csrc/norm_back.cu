@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? 2 : 1) norm_ba
     const u64 step = (u64)a.sets * a.groups, step_at = step * a.cols;
     u64 row = (u64)set * a.groups + rg.g, at = row * a.cols + c0;
     const bool more = a.dh_in != nullptr;
-    constexpr int STAGES = norm_stages(NV, THREADS);
+    constexpr int STAGES = norm_stages(NV, THREADS, TYPE);
     const Ring<TYPE, ALIGNED, NV, THREADS, STAGES> ring(dynamic, more ? 3u : 2u);
     float4 *params = reinterpret_cast<float4 *>(ring.end());
     float next_mean = 0.f, next_rstd = 0.f;
@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormMany ? 2 : 1) norm_ba
         if (a.cluster > 1) {
             cg::cluster_group cl = cg::this_cluster();
             if (threadIdx.x < a.cluster) cl.map_shared_rank(&peers[parity][0], threadIdx.x)[rank] = make_float2(s[0], s[1]);
-            cl.sync();
+            cluster_meet();
             s[0] = s[1] = 0.f;
             for (u32 j = 0; j < a.cluster; j++) {
                 s[0] += peers[parity][j].x;
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) norm_back_sum(const float *par
 
 template <u32 TYPE, bool ALIGNED, int NV, int THREADS> static void launch_drop(const NormArgs &a, cudaStream_t st)
 {
-    const size_t smem = Ring<TYPE, ALIGNED, NV, THREADS, norm_stages(NV, THREADS)>::bytes(a.dh_in ? 3u : 2u) + (NV == 1 ? 0 : (size_t)a.tpr * NV * 32);
+    const size_t smem = Ring<TYPE, ALIGNED, NV, THREADS, norm_stages(NV, THREADS, TYPE)>::bytes(a.dh_in ? 3u : 2u) + (NV == 1 ? 0 : (size_t)a.tpr * NV * 32);
     if (a.drop.threshold) launch_norm_kernel(norm_backward<TYPE, ALIGNED, NV, true, THREADS>, a, smem, st);
     else launch_norm_kernel(norm_backward<TYPE, ALIGNED, NV, false, THREADS>, a, smem, st);
 }

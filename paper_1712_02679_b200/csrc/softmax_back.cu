@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSoftShort ? soft_ctas(NV,
         if (a.cluster > 1) {
             cg::cluster_group cl = cg::this_cluster();
             if (threadIdx.x < a.cluster) cl.map_shared_rank(&peers[parity][0], threadIdx.x)[rows.rank] = v;
-            cl.sync();
+            cluster_meet();
             v = 0.f;
             for (u32 j = 0; j < a.cluster; j++) v += peers[parity][j];
         }
